@@ -11,7 +11,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 # (source, parts it is compiled in): the parts run side by side; the sources check that they are as many as they have
-SOURCES = [("het_cache.hip", 1), ("apply_variants.hip", 8), ("fill_variants.hip", 2)]
+SOURCES = [("het_cache.hip", 1), ("apply_variants.hip", 8), ("fill_variants.hip", 2), ("dense.hip", 1), ("dense_product.hip", 3)]
 OUT = os.path.join(HERE, "libhet_cache.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -23,10 +23,10 @@ FLAGS = [
 
 
 def source_id() -> str:
-    """Short hash of the sources the library is built from (the header and everything in csrc/):
+    """Short hash of the sources the library is built from (the headers and everything in csrc/):
     what `het_build_id()` returns, so that a measurement can name the build it was taken on."""
     h = hashlib.sha256()
-    files = [os.path.join(HERE, "..", "include", "het_cache.h")]
+    files = [os.path.join(HERE, "..", "include", h) for h in ("het_cache.h", "het_dense.h")]
     files += sorted(os.path.join(HERE, "csrc", f) for f in os.listdir(os.path.join(HERE, "csrc")))
     for f in files:
         with open(f, "rb") as fh:

@@ -1,0 +1,305 @@
+// Host side of include/het_dense.h: argument checks and launch shapes.  Nothing is allocated, nothing is kept from call to call.
+#include "../../include/het_dense.h"
+
+#include <algorithm>
+#include <cstdio>
+
+#include "dense_launch.hpp"
+#include "dense_rows.hpp"
+
+using namespace het;
+
+namespace {
+
+constexpr int64_t MOST_ROWS = (1ll << 31) - 1;
+constexpr int32_t MOST_DIM = 1 << 20;
+constexpr int64_t MOST_VALUES = 1ll << 40;          // of one matrix (terabytes): launches of a chunk a thread stay within a grid
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t align16(int64_t a) { return (a + 15) / 16 * 16; }
+int pitch_of(int dim) { return (dim + PACK_BLOCK - 1) / PACK_BLOCK * PACK_BLOCK; }
+int width_of(int dim) { return (dim + CHUNK - 1) / CHUNK * CHUNK; }
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+bool known_type(int32_t t) { return t == HET_F32 || t == HET_BF16 || t == HET_F16; }
+bool known_act(int32_t a) { return a >= HET_ACT_NONE && a <= HET_ACT_SILU; }
+int64_t size_of(int32_t t) { return t == HET_F32 ? 4 : 2; }
+
+int launched()
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return HET_OK;
+    std::fprintf(stderr, "het_dense: kernel launch: %s\n", hipGetErrorString(e));
+    return HET_EHIP;
+}
+
+struct Shape { RowShape s; int nv; bool block; };
+
+// Where a row of `dim` values lies (see RowShape).
+Shape shape_of(int dim)
+{
+    Shape h;
+    const int chunks = (int)cdiv(dim, CHUNK);
+    h.s.dim = dim; h.s.pitch = pitch_of(dim);
+    h.block = dim > ROW_WIDE;
+    if (h.block) {
+        h.s.lanes = dim <= 256 * CHUNK * 4 ? 256 : dim <= 512 * CHUNK * 4 ? 512 : 1024;
+    } else {
+        h.s.lanes = 4;
+        while (h.s.lanes < 64 && h.s.lanes < chunks) h.s.lanes *= 2;
+    }
+    const int n = (int)cdiv(chunks, h.s.lanes);
+    h.nv = n <= 1 ? 1 : n <= 2 ? 2 : 4;
+    return h;
+}
+
+int rows_per_group(const Shape &h) { return h.block ? 1 : ROW_THREADS / h.s.lanes; }
+
+int norm_groups(int64_t rows, const Shape &h) { return (int)std::min<int64_t>(PARTIALS, cdiv(rows, rows_per_group(h))); }
+
+template <typename TX, typename TY>
+void launch_norm(const NormArgs &a, const Shape &h, hipStream_t st)
+{
+    const dim3 grid((uint32_t)cdiv(a.rows, rows_per_group(h)));
+    if (h.block) {
+        if (h.nv == 2) norm_kernel<TX, TY, 2, true><<<grid, h.s.lanes, 0, st>>>(a);
+        else norm_kernel<TX, TY, 4, true><<<grid, h.s.lanes, 0, st>>>(a);
+    } else if (h.nv == 1) norm_kernel<TX, TY, 1, false><<<grid, ROW_THREADS, 0, st>>>(a);
+    else if (h.nv == 2) norm_kernel<TX, TY, 2, false><<<grid, ROW_THREADS, 0, st>>>(a);
+    else norm_kernel<TX, TY, 4, false><<<grid, ROW_THREADS, 0, st>>>(a);
+}
+
+template <typename TX, typename TY>
+void launch_norm_back(const NormBackArgs &a, const Shape &h, int groups, hipStream_t st)
+{
+    const size_t lds = h.block ? 0 : 2 * (size_t)width_of(h.s.dim) * sizeof(float);
+    if (h.block) {
+        if (h.nv == 2) norm_back_kernel<TX, TY, 2, true><<<groups, h.s.lanes, lds, st>>>(a);
+        else norm_back_kernel<TX, TY, 4, true><<<groups, h.s.lanes, lds, st>>>(a);
+    } else if (h.nv == 1) norm_back_kernel<TX, TY, 1, false><<<groups, ROW_THREADS, lds, st>>>(a);
+    else if (h.nv == 2) norm_back_kernel<TX, TY, 2, false><<<groups, ROW_THREADS, lds, st>>>(a);
+    else norm_back_kernel<TX, TY, 4, false><<<groups, ROW_THREADS, lds, st>>>(a);
+}
+
+void launch_column_sum(const float *partial, int n, int sets, int dim, float *out0, float *out1, hipStream_t st)
+{
+    ColumnSumArgs s;
+    s.partial = partial; s.out[0] = out0; s.out[1] = out1;
+    s.n = n; s.sets = sets; s.width = width_of(dim); s.dim = dim;
+    column_sum_kernel<<<(uint32_t)cdiv((int64_t)sets * s.width, 16), 256, 0, st>>>(s);
+}
+
+// f(tag of x's type, tag of y's type); false: no such pair.
+template <typename T> struct Tag { using type = T; };
+template <typename F>
+bool with_types(int32_t x, int32_t y, F &&f)
+{
+    if (x == HET_F32) {
+        if (y == HET_F32) f(Tag<float>(), Tag<float>());
+        else if (y == HET_BF16) f(Tag<float>(), Tag<bf16>());
+        else f(Tag<float>(), Tag<f16>());
+        return true;
+    }
+    if (x != y) return false;
+    if (x == HET_BF16) f(Tag<bf16>(), Tag<bf16>());
+    else f(Tag<f16>(), Tag<f16>());
+    return true;
+}
+template <typename F>
+void with_type(int32_t t, F &&f)
+{
+    if (t == HET_F32) f(Tag<float>());
+    else if (t == HET_BF16) f(Tag<bf16>());
+    else f(Tag<f16>());
+}
+bool known_pair(int32_t x, int32_t y) { return known_type(x) && known_type(y) && (x == y || x == HET_F32); }
+
+bool pack_sizes(int64_t rows, int32_t dim) { return rows >= 0 && rows <= MOST_ROWS && dim >= 1 && dim <= MOST_DIM && rows * dim <= MOST_VALUES; }
+bool norm_sizes(int64_t rows, int32_t dim) { return dim >= 1 && dim <= ROW_WIDEST && rows >= 0 && rows <= MOST_ROWS; }
+
+// ---- linear layers ------------------------------------------------------------------------------------
+bool linear_sizes(const het_linear_t *l)
+{
+    return l && l->rows >= 0 && l->rows <= MOST_ROWS - 255 && l->in >= 1 && l->in <= MOST_DIM && l->out >= 1 && l->out <= MOST_DIM && known_type(l->type) &&
+           l->rows * std::max(l->in, l->out) <= MOST_VALUES;
+}
+
+int slope_splits(int64_t rows, int32_t out)
+{
+    // enough workgroups to fill the chip, at least 32 rows for each
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)PARTIALS, cdiv(rows, 32), cdiv(2048, cdiv(out, SLOPE_COLS))}));
+}
+
+struct BackPlan {
+    ProductPlan dx, dw;
+    int slope;                  // workgroups down the rows
+    int64_t bias_at, x_at, partial_at, bytes;
+};
+
+BackPlan back_plan(const het_linear_t *l)
+{
+    BackPlan p;
+    p.dx = product_plan(l->rows, l->in, l->out, l->type, true, false);
+    p.dw = product_plan(l->out, l->in, l->rows, l->type, false, false);
+    p.slope = slope_splits(l->rows, l->out);
+    p.bias_at = 0;
+    p.x_at = l->dbias ? align16((int64_t)p.slope * width_of(l->out) * 4) : 0;
+    p.partial_at = p.x_at + (l->xq && l->dw ? align16(l->rows * (int64_t)l->in * size_of(l->type)) : 0);
+    p.bytes = p.partial_at + std::max(l->dx ? p.dx.partial_bytes : 0, l->dw ? p.dw.partial_bytes : 0);
+    return p;
+}
+
+bool workspace_ok(const void *ws, int64_t have, int64_t need) { return need == 0 || (ws && aligned16(ws) && have >= need); }
+
+} // namespace
+
+extern "C" {
+
+int het_layer_norm(const void *x, int32_t x_type, int64_t ldx, const float *gamma, const float *beta, void *y, int32_t y_type,
+                   int64_t ldy, float *mean, float *rstd, int8_t *q, uint8_t *e, int64_t rows, int32_t dim, float eps, void *hip_stream)
+{
+    if (!norm_sizes(rows, dim) || !known_pair(x_type, y_type) || !(eps >= 0.f) || ldx < dim || ldy < dim || !q != !e) return HET_EINVAL;
+    if (rows == 0) return HET_OK;
+    if (!x || !y || !aligned16(q)) return HET_EINVAL;
+    const Shape h = shape_of(dim);
+    NormArgs a{x, gamma, beta, y, mean, rstd, q, e, ldx, ldy, rows, h.s, eps};
+    with_types(x_type, y_type, [&](auto tx, auto ty) {
+        launch_norm<typename decltype(tx)::type, typename decltype(ty)::type>(a, h, static_cast<hipStream_t>(hip_stream));
+    });
+    return launched();
+}
+
+int64_t het_layer_norm_workspace(int64_t rows, int32_t dim)
+{
+    if (!norm_sizes(rows, dim)) return HET_EINVAL;
+    return (int64_t)norm_groups(rows, shape_of(dim)) * 2 * width_of(dim) * 4;
+}
+
+int het_layer_norm_backward(const void *dy, int32_t y_type, int64_t lddy, const void *x, int32_t x_type, int64_t ldx,
+                            const float *mean, const float *rstd, const int8_t *q, const uint8_t *e, const float *gamma,
+                            const void *residual, int64_t ld_residual, void *dx, int64_t lddx, float *dgamma, float *dbeta,
+                            int64_t rows, int32_t dim, void *workspace, int64_t workspace_bytes, void *hip_stream)
+{
+    if (!norm_sizes(rows, dim) || !known_pair(x_type, y_type) || lddy < dim || lddx < dim || !q != !e) return HET_EINVAL;
+    if ((!q && ldx < dim) || (residual && ld_residual < dim)) return HET_EINVAL;
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    if (rows > 0 && (!dy || !dx || !rstd || (!q && (!x || !mean)) || !aligned16(q))) return HET_EINVAL;
+    if (!workspace_ok(workspace, workspace_bytes, het_layer_norm_workspace(rows, dim))) return HET_EINVAL;
+    if (rows == 0 && !dgamma && !dbeta) return HET_OK;
+    const Shape h = shape_of(dim);
+    const int groups = norm_groups(rows, h);
+    float *partial = static_cast<float *>(workspace);
+    if (rows > 0) {
+        NormBackArgs a{dy, x, mean, rstd, q, e, gamma, residual, dx, partial, lddy, ldx, ld_residual, lddx, rows, h.s};
+        with_types(x_type, y_type, [&](auto tx, auto ty) { launch_norm_back<typename decltype(tx)::type, typename decltype(ty)::type>(a, h, groups, st); });
+    }
+    if (dgamma || dbeta) launch_column_sum(partial, groups, 2, dim, dgamma, dbeta, st);
+    return launched();
+}
+
+int het_pack(const void *x, int32_t type, int64_t ldx, int8_t *q, uint8_t *e, int64_t rows, int32_t dim, void *hip_stream)
+{
+    if (!pack_sizes(rows, dim) || !known_type(type) || ldx < dim) return HET_EINVAL;
+    if (rows == 0) return HET_OK;
+    const int64_t blocks = cdiv(rows * (pitch_of(dim) / CHUNK), 256);
+    if (!x || !q || !e || !aligned16(q)) return HET_EINVAL;
+    PackArgs a{x, q, e, ldx, rows, dim, pitch_of(dim)};
+    with_type(type, [&](auto t) { pack_kernel<typename decltype(t)::type><<<(uint32_t)blocks, 256, 0, static_cast<hipStream_t>(hip_stream)>>>(a); });
+    return launched();
+}
+
+int het_expand(const int8_t *q, const uint8_t *e, int64_t rows, int32_t dim, const float *gamma, const float *beta, int32_t act,
+               void *y, int32_t type, int64_t ldy, void *hip_stream)
+{
+    if (!pack_sizes(rows, dim) || !known_type(type) || !known_act(act) || ldy < dim) return HET_EINVAL;
+    if (rows == 0) return HET_OK;
+    const int64_t blocks = cdiv(rows * cdiv(dim, CHUNK), 256);
+    if (!y || !q || !e || !aligned16(q)) return HET_EINVAL;
+    ExpandArgs a{q, e, gamma, beta, y, ldy, rows, dim, pitch_of(dim), act};
+    with_type(type, [&](auto t) { expand_kernel<typename decltype(t)::type><<<(uint32_t)blocks, 256, 0, static_cast<hipStream_t>(hip_stream)>>>(a); });
+    return launched();
+}
+
+int64_t het_linear_workspace(const het_linear_t *l, int32_t backward)
+{
+    if (!linear_sizes(l)) return HET_EINVAL;
+    if (backward) return back_plan(l).bytes;
+    return product_plan(l->rows, l->out, l->in, l->type, true, true).partial_bytes;
+}
+
+int het_linear(const het_linear_t *l, void *hip_stream)
+{
+    if (!linear_sizes(l) || !known_act(l->act) || (l->y_type != l->type && l->y_type != HET_F32)) return HET_EINVAL;
+    if (l->ldx < l->in || l->ldw < l->in || l->ldy < l->out || (l->residual && l->ld_residual < l->out) || (l->z && l->ldz < l->out) || !l->zq != !l->ze) return HET_EINVAL;
+    if (l->rows == 0) return HET_OK;
+    if (!l->x || !l->w || !l->y || !aligned16(l->zq)) return HET_EINVAL;
+    const ProductPlan p = product_plan(l->rows, l->out, l->in, l->type, true, true);
+    if (!p.ok || !workspace_ok(l->workspace, l->workspace_bytes, p.partial_bytes)) return HET_EINVAL;
+    ProductArgs a{};
+    a.a = l->x; a.lda = l->ldx; a.b = l->w; a.ldb = l->ldw;
+    a.partial = static_cast<float *>(l->workspace);
+    a.f.bias = l->bias;
+    a.f.residual = l->residual; a.f.ldr = l->ld_residual;
+    a.f.y = l->y; a.f.ldy = l->ldy;
+    a.f.z = l->z; a.f.ldz = l->ldz;
+    a.f.q = l->zq; a.f.e = l->ze; a.f.pitch = pitch_of(l->out);
+    a.f.act = l->act;
+    a.f.y_f32 = l->y_type == HET_F32;
+    launch_product(a, p, l->type, true, true, static_cast<hipStream_t>(hip_stream));
+    return launched();
+}
+
+int het_linear_backward(const het_linear_t *l, void *hip_stream)
+{
+    if (!linear_sizes(l) || !known_act(l->act) || !known_act(l->x_act) || (l->y_type != l->type && l->y_type != HET_F32)) return HET_EINVAL;
+    const bool has_act = l->act != HET_ACT_NONE, some = l->rows > 0;
+    const bool dz_is_dy = !l->dz;
+    if (some && dz_is_dy && (has_act || l->y_type != l->type)) return HET_EINVAL;
+    if (l->lddy < l->out || (l->dz && l->lddz < l->out)) return HET_EINVAL;
+    if (has_act && (!l->zq != !l->ze || (some && !l->zq && l->ldz < l->out))) return HET_EINVAL;
+    if (l->dx && (l->lddx < l->in || l->ldw < l->in)) return HET_EINVAL;
+    if (l->dw && (l->lddw < l->in || !l->xq != !l->xe || (some && !l->xq && l->ldx < l->in))) return HET_EINVAL;
+    if (some) {
+        if (!l->dy || (has_act && !l->zq && !l->z) || (has_act && !aligned16(l->zq))) return HET_EINVAL;
+        if ((l->dx && !l->w) || (l->dw && !l->xq && !l->x) || (l->dw && !aligned16(l->xq))) return HET_EINVAL;
+    }
+    const BackPlan p = back_plan(l);
+    if ((l->dx && !p.dx.ok) || (l->dw && !p.dw.ok) || !workspace_ok(l->workspace, l->workspace_bytes, p.bytes)) return HET_EINVAL;
+    if (!some && !l->dw && !l->dbias) return HET_OK;
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    char *ws = static_cast<char *>(l->workspace);
+    if (l->dz || l->dbias) {
+        SlopeArgs s{};
+        s.dy = l->dy; s.lddy = l->lddy;
+        s.z = l->z; s.ldz = l->ldz; s.q = l->zq; s.e = l->ze;
+        s.dz = l->dz; s.lddz = l->lddz;
+        s.partial = l->dbias ? reinterpret_cast<float *>(ws + p.bias_at) : nullptr;
+        s.rows = l->rows; s.dim = l->out; s.pitch = pitch_of(l->out); s.act = l->act;
+        const dim3 grid((uint32_t)cdiv(l->out, SLOPE_COLS), (uint32_t)p.slope);
+        with_types(l->y_type, l->type, [&](auto ty, auto t) { slope_kernel<typename decltype(t)::type, typename decltype(ty)::type><<<grid, 256, 0, st>>>(s); });
+        if (l->dbias) launch_column_sum(s.partial, p.slope, 1, l->out, l->dbias, nullptr, st);
+    }
+    const void *dz = dz_is_dy ? l->dy : l->dz;
+    const int64_t lddz = dz_is_dy ? l->lddy : l->lddz;
+    if (l->dx && some) {
+        ProductArgs a{};
+        a.a = dz; a.lda = lddz; a.b = l->w; a.ldb = l->ldw;
+        a.partial = reinterpret_cast<float *>(ws + p.partial_at);
+        a.f.y = l->dx; a.f.ldy = l->lddx; a.f.y_f32 = l->type == HET_F32;
+        launch_product(a, p.dx, l->type, true, false, st);
+    }
+    if (l->dw) {
+        if (l->xq && some) {
+            const int rc = het_expand(l->xq, l->xe, l->rows, l->in, l->x_gamma, l->x_beta, l->x_act, ws + p.x_at, l->type, l->in, hip_stream);
+            if (rc != HET_OK) return rc;
+        }
+        ProductArgs a{};
+        a.a = dz; a.lda = lddz;
+        a.b = l->xq ? static_cast<const void *>(ws + p.x_at) : l->x; a.ldb = l->xq ? l->in : l->ldx;
+        a.partial = reinterpret_cast<float *>(ws + p.partial_at);
+        a.f.y = l->dw; a.f.ldy = l->lddw; a.f.y_f32 = l->type == HET_F32;
+        launch_product(a, p.dw, l->type, false, false, st);
+    }
+    return launched();
+}
+
+} // extern "C"

@@ -1,0 +1,366 @@
+// Matrix products of the dense layers on the matrix cores, with what follows them (bias, activation, residual, 8-bit copy) done while the
+// sums are still in registers.
+//
+// All are D[m][n] = sum over k of A(m, k) B(n, k).  An operand is read along k (K: its rows are A's or B's, as x and w are in x w^T) or
+// across (its rows are k's, as w is in dz w, and both are in dz^T x); nothing is transposed in memory.
+#pragma once
+#include "dense_types.hpp"
+
+namespace het {
+
+// What becomes of a sum: z = sum + bias is kept where the backward pass needs it, y = act(z) + residual.
+struct Finish {
+    const float *bias;        // null: none
+    const void *residual;     // of y's type, or null
+    void *y;
+    void *z;                  // z in the operands' type, or null
+    int8_t *q;                // z in 8 bits, or null
+    uint8_t *e;
+    int64_t ldr, ldy, ldz;
+    int pitch, act;
+    int y_f32;                // y and residual are fp32 whatever the operands are
+};
+
+struct ProductArgs {
+    const void *a, *b;
+    int64_t lda, ldb;
+    int m, n, k;
+    int tiles_m, tiles_n;
+    int splits, k_split;      // the k's of a workgroup: k_split of them, a multiple of the kernel's step
+    float *partial;           // splits > 1: [split][m][n rounded up to 16], joined by join_kernel
+    Finish f;
+};
+
+__device__ __forceinline__ int partial_width(int n) { return (n + 15) & ~15; }
+
+template <typename TY>
+__device__ __forceinline__ void finish_store(const Finish &f, int64_t row, int col, int n, f32x8 v)
+{
+    if (f.residual) {
+        const f32x8 r = load_some(static_cast<const TY *>(f.residual) + row * f.ldr + col, n);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += r[j];
+    }
+    store_some(static_cast<TY *>(f.y) + row * f.ldy + col, v, n);
+}
+
+// z of a chunk at (row, col), n of its values in the matrix.  Values behind the row's end are zero.
+__device__ __forceinline__ f32x8 finish_bias(const Finish &f, int col, int n, f32x8 v)
+{
+    if (f.bias && n > 0) {
+        const f32x8 b = load_some(f.bias + col, n);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += b[j];
+    }
+    return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void finish_value(const Finish &f, int64_t row, int col, int n, f32x8 v)
+{
+    if (n <= 0) return;
+    if (f.z) store_some(static_cast<T *>(f.z) + row * f.ldz + col, v, n);
+    if (f.act != DENSE_ACT_NONE)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = act_value(f.act, v[j]);
+    if (f.y_f32) finish_store<float>(f, row, col, n, v);
+    else finish_store<T>(f, row, col, n, v);
+}
+
+// ---- operands in LDS ------------------------------------------------------------------------------------
+// A step takes 128 bytes of k from each row of a tile: 64 values of 16 bits, 32 of fp32.  The matrix instructions take 16 bytes of k a lane
+// (`frag`): one 32x32x16 product of 16-bit values, or four 32x32x2 products of fp32, so a step is four frags in either case.
+//
+// The first operand of an instruction is B, the second A: a lane then holds one row of D and 16 columns.  Which row of the tile stands at
+// which of the instruction's 32 rows is free; B's stand so that these 16 columns are neighbours (col_of).
+template <typename T> struct Frag;
+template <> struct Frag<bf16> { using type = vec<bf16, 8>; };
+template <> struct Frag<f16> { using type = vec<f16, 8>; };
+template <> struct Frag<float> { using type = f32x4; };
+
+__device__ __forceinline__ f32x16 multiply(vec<bf16, 8> a, vec<bf16, 8> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 multiply(vec<f16, 8> a, vec<f16, 8> b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x16 multiply(f32x4 a, f32x4 b, f32x16 c)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+__device__ __forceinline__ f32x4 multiply_small(vec<bf16, 8> a, vec<bf16, 8> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 multiply_small(vec<f16, 8> a, vec<f16, 8> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 multiply_small(f32x4 a, f32x4 b, f32x4 c)
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+}
+
+// The instruction's row i of 32 -> column of D within the tile's 32: lane half h holds rows 8 (v / 4) + 4 h + v % 4 of the result (v = 0 .. 15),
+// which are to be the columns 16 h + v.
+__device__ __forceinline__ int col_of(int i) { return 16 * ((i >> 2) & 1) + 4 * (i >> 3) + (i & 3); }
+
+// An operand's tile in LDS: R rows and 128 bytes of k.
+//   K:  [row][128 bytes], pieces of 16 bytes;  across:  [k][R values].
+// The order of the pieces within 128 (or 64 R / 32 ...) bytes is mixed by row or k, so that the lanes of a read meet all banks.
+template <typename T, int R, bool K, bool PERMUTED>
+struct Tile {
+    static constexpr int PIECE = 16 / (int)sizeof(T);             // values of a piece
+    static constexpr int STEP = 128 / (int)sizeof(T);             // k's of a step
+    static constexpr int PIECES = R * 8;
+    static constexpr int WIDE = K ? 8 : R / PIECE;                // pieces of a row of the tile in LDS
+    using F = typename Frag<T>::type;
+
+    __device__ static __forceinline__ int mixed(int r, int c)     // place of piece c of row (or k) r
+    {
+        if (K) return r * 8 + (c ^ (PERMUTED ? (r & 3) | ((r >> 2) & 4) : r & 7));
+        if (sizeof(T) == 2) return r * WIDE + (c ^ (4 * (r & 3)));
+        return r * WIDE + (c ^ (8 * ((r >> 2) & 1)));
+    }
+    // Piece `i` of the tile (0 .. PIECES - 1) from memory: rows [row0, rows), k's [k0, k_end); what lies outside is zero.
+    __device__ static __forceinline__ i32x4 load(const T *p, int64_t ld, int i, int row0, int rows, int k0, int k_end)
+    {
+        const int along = i % WIDE, down = i / WIDE;
+        const int outer = (K ? row0 : k0) + down, inner = (K ? k0 : row0) + along * PIECE;
+        const int left = (K ? k_end : rows) - inner;
+        vec<T, PIECE> v = {};
+        if (outer < (K ? rows : k_end) && left > 0) {
+            const T *at = p + (int64_t)outer * ld + inner;
+            if (left >= PIECE) {
+                __builtin_memcpy(&v, at, 16);
+            } else {
+#pragma unroll
+                for (int j = 0; j < PIECE - 1; ++j) if (j < left) v[j] = at[j];
+            }
+        }
+        return __builtin_bit_cast(i32x4, v);
+    }
+    __device__ static __forceinline__ int place(int i) { return mixed(i / WIDE, i % WIDE); }
+
+    // Frag `s` (0 .. 3) of the 32 rows from r0.
+    __device__ static __forceinline__ F read(const i32x4 *lds, int r0, int s)
+    {
+        const int lane = threadIdx.x % 64, h = lane / 32;
+        if (K) {
+            const int r = r0 + (PERMUTED ? col_of(lane % 32) : lane % 32);
+            return __builtin_bit_cast(F, lds[mixed(r, 2 * s + h)]);
+        }
+        return across(lds, r0, s, F{});
+    }
+    // 16 bits, across: two transposing reads.  In each, the 16 lanes of a group name 4 k's of 16 rows, 4 values a lane, and every lane gets the 4 k's of
+    // one row.
+    template <typename V>
+    __device__ static __forceinline__ V across(const i32x4 *lds, int r0, int s, V)
+    {
+        using S = vec<short, 4>;
+        using P = __attribute__((address_space(3))) S *;
+        const int lane = threadIdx.x % 64, g = lane / 16, i = lane % 16, k = 16 * s + 8 * (g / 2) + i / 4;
+        const int in = 16 * (g % 2) + 4 * (i % 4), r = r0 + (PERMUTED ? col_of(in) : in);
+        const char *base = reinterpret_cast<const char *>(lds);
+        const S lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(base + mixed(k, r / 8) * 16 + r % 8 * 2));
+        const S hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(base + mixed(k + 4, r / 8) * 16 + r % 8 * 2));
+        return __builtin_bit_cast(V, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    __device__ static __forceinline__ f32x4 across(const i32x4 *lds, int r0, int s, f32x4)
+    {
+        const int lane = threadIdx.x % 64, k = 8 * s + 4 * (lane / 32), r = r0 + (PERMUTED ? col_of(lane % 32) : lane % 32);
+        const float *base = reinterpret_cast<const float *>(lds);
+        f32x4 v;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = base[mixed(k + j, r / 4) * 4 + r % 4];
+        return v;
+    }
+};
+
+// Workgroups are handed to the 8 XCDs in turn; each gets a run of neighbouring tiles, whose operands its own L2 then holds.
+__device__ __forceinline__ int tile_of(int block, int tiles)
+{
+    const int x = block % 8, each = tiles / 8, more = tiles % 8;
+    return x * each + (x < more ? x : more) + block / 8;
+}
+
+// Tiles in bands of 8 rows of tiles: neighbours share A's rows or B's.
+__device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    const int band = t / (8 * tiles_n), first = band * 8, high = tiles_m - first < 8 ? tiles_m - first : 8, in = t - band * 8 * tiles_n;
+    tm = first + in % high;
+    tn = in / high;
+}
+
+// Ends a wave's 32 x 32 sums at (row0, col0): 16 columns a lane.
+template <typename T>
+__device__ __forceinline__ void finish_tile(const ProductArgs &a, int split, int row0, int col0, const f32x16 &acc)
+{
+    const int lane = threadIdx.x % 64, row = row0 + lane % 32, col = col0 + 16 * (lane / 32);
+    if (row >= a.m || col0 >= a.n) return;
+    f32x8 v[2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { v[0][j] = acc[j]; v[1][j] = acc[8 + j]; }
+    if (a.splits > 1) {
+        const int width = partial_width(a.n);
+        if (col >= width) return;
+        float *p = a.partial + ((int64_t)split * a.m + row) * width + col;
+        store_chunk(p, v[0]);
+        store_chunk(p + 8, v[1]);
+        return;
+    }
+    v[0] = finish_bias(a.f, col, a.n - col, v[0]);
+    v[1] = finish_bias(a.f, col + 8, a.n - col - 8, v[1]);
+    if (a.f.q) {
+        uint32_t most = chunk_magnitude(v[0]);
+        const uint32_t o = chunk_magnitude(v[1]);
+        most = most > o ? most : o;
+        const uint32_t other = __shfl_xor(most, 32);
+        const PackStep s = pack_step(most > other ? most : other);
+        uint4 w;
+        w.x = pack_four(v[0][0], v[0][1], v[0][2], v[0][3], s); w.y = pack_four(v[0][4], v[0][5], v[0][6], v[0][7], s);
+        w.z = pack_four(v[1][0], v[1][1], v[1][2], v[1][3], s); w.w = pack_four(v[1][4], v[1][5], v[1][6], v[1][7], s);
+        *reinterpret_cast<uint4 *>(a.f.q + (int64_t)row * a.f.pitch + col) = w;
+        if (lane < 32) a.f.e[(int64_t)row * (a.f.pitch / PACK_BLOCK) + col0 / PACK_BLOCK] = (uint8_t)s.byte;
+    }
+    finish_value<T>(a.f, row, col, a.n - col, v[0]);
+    finish_value<T>(a.f, row, col + 8, a.n - col - 8, v[1]);
+}
+
+// ---- any size, any stride ---------------------------------------------------------------------------------
+// 128 x 128 tiles, four waves of 64 x 64.  Pieces go through registers, where edges are cut off: the next step's are under way while this one's are multiplied.
+constexpr int ANY_TILE = 128;
+
+template <typename T, bool AK, bool BK>
+__global__ __launch_bounds__(256) void product_any_kernel(ProductArgs a)
+{
+    using TA = Tile<T, ANY_TILE, AK, false>;
+    using TB = Tile<T, ANY_TILE, BK, true>;
+    __shared__ i32x4 la[TA::PIECES], lb[TB::PIECES];
+    const int tiles = a.tiles_m * a.tiles_n, split = blockIdx.x / tiles;
+    int tm, tn;
+    tile_at(tile_of(blockIdx.x % tiles, tiles), a.tiles_m, a.tiles_n, tm, tn);
+    const int row0 = tm * ANY_TILE, col0 = tn * ANY_TILE;
+    const int k_begin = split * a.k_split, k_end = a.k - k_begin < a.k_split ? a.k : k_begin + a.k_split;
+    const T *pa = static_cast<const T *>(a.a), *pb = static_cast<const T *>(a.b);
+    const int wave = threadIdx.x / 64, wm = (wave / 2) * 64, wn = (wave % 2) * 64;
+
+    i32x4 ra[4], rb[4];
+    auto fetch = [&](int k0) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            ra[u] = TA::load(pa, a.lda, threadIdx.x + u * 256, row0, a.m, k0, k_end);
+            rb[u] = TB::load(pb, a.ldb, threadIdx.x + u * 256, col0, a.n, k0, k_end);
+        }
+    };
+    f32x16 acc[2][2] = {};
+    if (k_begin < k_end) fetch(k_begin);
+    for (int k0 = k_begin; k0 < k_end; k0 += TA::STEP) {
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < 4; ++u) { la[TA::place(threadIdx.x + u * 256)] = ra[u]; lb[TB::place(threadIdx.x + u * 256)] = rb[u]; }
+        __syncthreads();
+        if (k0 + TA::STEP < k_end) fetch(k0 + TA::STEP);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            typename TA::F fa[2];
+            typename TB::F fb[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { fa[i] = TA::read(la, wm + 32 * i, s); fb[i] = TB::read(lb, wn + 32 * i, s); }
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[i][j] = multiply(fb[j], fa[i], acc[i][j]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) finish_tile<T>(a, split, row0 + wm + 32 * i, col0 + wn + 32 * j, acc[i][j]);
+}
+
+// Adds the splits' sums in their order and ends them.  A chunk a thread, four for each block of 32 columns (the 8-bit copy needs them side by side).
+template <typename T>
+__global__ __launch_bounds__(256) void join_kernel(ProductArgs a)
+{
+    const int width = partial_width(a.n), per = (a.n + PACK_BLOCK - 1) / PACK_BLOCK * 4;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+    if (row >= a.m) return;
+    const int c = (int)(i - row * per), col = c * CHUNK, n = a.n - col;
+    f32x8 v = {};
+    if (n > 0) {
+        const float *p = a.partial + row * width + col;
+        for (int s = 0; s < a.splits; ++s) {
+            const f32x8 x = load_chunk(p + (int64_t)s * a.m * width);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += x[j];
+        }
+    }
+    v = finish_bias(a.f, col, n, v);
+    if (a.f.q) pack_chunk(a.f.q + row * a.f.pitch, a.f.e + row * (a.f.pitch / PACK_BLOCK), c, v);
+    finish_value<T>(a.f, row, col, n, v);
+}
+
+// ---- few rows ---------------------------------------------------------------------------------------------
+// Up to 16 MT rows (a request's candidates, a single token): bound by reading w once.  A workgroup takes 16 NT rows of w, its waves share
+// k; operands go from memory into the matrix instructions' registers, and the waves' sums meet in LDS.
+constexpr int FEW_WAVES = 8;
+
+template <typename T, int MT, int NT>
+__global__ __launch_bounds__(64 * FEW_WAVES) void product_few_kernel(ProductArgs a)
+{
+    constexpr int PIECE = 16 / (int)sizeof(T), SPAN = 4 * PIECE;        // k's of a lane's piece, and of an instruction's four pieces
+    using F = typename Frag<T>::type;
+    __shared__ float lds[FEW_WAVES][16 * MT][16 * NT + 4];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16, col0 = blockIdx.x * 16 * NT;
+    const T *pa[MT], *pb[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) pa[i] = static_cast<const T *>(a.a) + (int64_t)(16 * i + r < a.m ? 16 * i + r : 0) * a.lda;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) pb[i] = static_cast<const T *>(a.b) + (int64_t)(col0 + 16 * i + r < a.n ? col0 + 16 * i + r : 0) * a.ldb;
+    f32x4 acc[MT][NT] = {};
+    const int whole = a.k / SPAN;                     // instructions' spans without an edge
+#pragma unroll 4
+    for (int t = wave; t < whole; t += FEW_WAVES) {
+        const int k = t * SPAN + g * PIECE;
+        F fa[MT], fb[NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) __builtin_memcpy(&fb[i], pb[i] + k, 16);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) __builtin_memcpy(&fa[i], pa[i] + k, 16);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = multiply_small(fb[j], fa[i], acc[i][j]);
+    }
+    if (whole * SPAN < a.k && wave == whole % FEW_WAVES) {
+        const int k = whole * SPAN + g * PIECE, left = a.k - k;
+        F fa[MT], fb[NT];
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+#pragma unroll
+            for (int j = 0; j < PIECE; ++j) fb[i][j] = j < left ? pb[i][k + j] : (T)0.f;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < PIECE; ++j) fa[i][j] = j < left ? pa[i][k + j] : (T)0.f;
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = multiply_small(fb[j], fa[i], acc[i][j]);
+    }
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4 *>(&lds[wave][16 * i + r][16 * j + 4 * g]) = acc[i][j];
+    __syncthreads();
+    const int c = threadIdx.x % (2 * NT), row = threadIdx.x / (2 * NT);
+    if (row >= 16 * MT || row >= a.m) return;
+    const int col = col0 + c * CHUNK, n = a.n - col;
+    f32x8 v = {};
+#pragma unroll
+    for (int w = 0; w < FEW_WAVES; ++w)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += lds[w][row][c * CHUNK + j];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? v[j] : 0.f;      // (rows of w behind the last one were read as its first)
+    v = finish_bias(a.f, col, n, v);
+    if (NT == 2 && a.f.q) pack_chunk(a.f.q + (int64_t)row * a.f.pitch, a.f.e + (int64_t)row * (a.f.pitch / PACK_BLOCK), col / CHUNK, v);
+    finish_value<T>(a.f, row, col, n, v);
+}
+
+} // namespace het

@@ -1,0 +1,395 @@
+// Row-wise kernels of the dense layers: layer norm, its backward pass, the slope of an activation with the bias' gradient, and the
+// 8-bit form of activations.  All are bound by HBM (or, where rows are few, by a launch): every value is read once, kept in
+// registers while its row's sums are formed, and written once.
+#pragma once
+#include "dense_types.hpp"
+
+namespace het {
+
+constexpr int ROW_THREADS = 256;
+constexpr int ROW_WAVES = ROW_THREADS / 64;
+constexpr int ROW_WIDE = 64 * CHUNK * 4;           // widest row that a wave holds: 4 chunks a lane
+constexpr int ROW_WIDEST = 1024 * CHUNK * 4;       // and a workgroup
+constexpr uint32_t PARTIALS = 512;                 // workgroups that leave partial column sums
+
+// How a row lies over lanes.  Rows of up to ROW_WIDE values belong to `lanes` (a power of two, at least a block's four) consecutive lanes of
+// a wave, wider ones to a whole workgroup; lane l holds the chunks l, l + lanes, ...
+struct RowShape {
+    int dim;           // values of a row
+    int pitch;         // ... in the 8-bit form: rounded up to whole blocks
+    int lanes;         // lanes of a row, or threads of a workgroup that holds one
+};
+
+// Sum over the `lanes` lanes of a row; every lane gets it, all the same bits (each step adds two equal sums' worth in either order).
+__device__ __forceinline__ float lanes_sum(float v, int lanes)
+{
+    v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0xB1, 0xf, 0xf, false));       // lanes 1 0 3 2
+    v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x4E, 0xf, 0xf, false));       // lanes 2 3 0 1
+    if (lanes >= 8) v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x141, 0xf, 0xf, false));    // mirrored in 8
+    if (lanes >= 16) v += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x140, 0xf, 0xf, false));   // mirrored in 16
+    if (lanes >= 32) v += __shfl_xor(v, 16);
+    if (lanes >= 64) v += __shfl_xor(v, 32);
+    return v;
+}
+
+// The sums of a row: over its lanes, or over the workgroup (`lds`: 32 floats; calls alternate between two areas, so one barrier does).
+template <bool BLOCK>
+struct RowSum {
+    float *lds;
+    int lanes;
+    int turn = 0;
+    __device__ __forceinline__ RowSum(float *lds_, int lanes_) : lds(lds_), lanes(lanes_) {}
+    // Two sums at once: one trip.
+    __device__ __forceinline__ void two(float &a, float &b)
+    {
+        a = lanes_sum(a, BLOCK ? 64 : lanes);
+        b = lanes_sum(b, BLOCK ? 64 : lanes);
+        if (!BLOCK) return;
+        float *at = lds + 32 * turn;
+        turn ^= 1;
+        const int w = threadIdx.x / 64, waves = lanes / 64;
+        if (threadIdx.x % 64 == 0) { at[w] = a; at[16 + w] = b; }
+        __syncthreads();
+        a = at[0]; b = at[16];
+        for (int i = 1; i < waves; ++i) { a += at[i]; b += at[16 + i]; }
+    }
+    __device__ __forceinline__ float one(float a) { float b = 0.f; two(a, b); return a; }
+};
+
+__device__ __forceinline__ int chunk_values(int c, int dim)      // values of chunk c that are in the row
+{
+    const int n = dim - c * CHUNK;
+    return n < 0 ? 0 : n;
+}
+
+// ---- layer norm ---------------------------------------------------------------------------------------
+// y = gamma (x - mean) rstd + beta, rstd = 1 / sqrt(var + eps).  The variance is summed from the differences to the mean (the row is in
+// registers), not as a difference of two large sums.  All sums in 32 bits.
+struct NormArgs {
+    const void *x;
+    const float *gamma, *beta;
+    void *y;
+    float *mean, *rstd;
+    int8_t *q;              // normalised rows in 8 bits, or null
+    uint8_t *e;
+    int64_t ldx, ldy, rows;
+    RowShape s;
+    float eps;
+};
+
+template <typename TX, typename TY, int NV, bool BLOCK>
+__global__ __launch_bounds__(BLOCK ? 1024 : ROW_THREADS) void norm_kernel(NormArgs a)
+{
+    __shared__ float lds[64];
+    const int lanes = a.s.lanes, gl = threadIdx.x % lanes, dim = a.s.dim;
+    const int64_t row = BLOCK ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (ROW_THREADS / lanes) + threadIdx.x / lanes;
+    if (row >= a.rows) return;                     // (whole rows of lanes; a workgroup that holds one row has one)
+    const TX *x = static_cast<const TX *>(a.x) + row * a.ldx;
+    RowSum<BLOCK> sum(lds, lanes);
+    f32x8 v[NV];
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = gl + i * lanes, n = chunk_values(c, dim);
+        v[i] = n > 0 ? load_some(x + c * CHUNK, n) : f32x8{};
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += v[i][j];
+    const float mean = sum.one(s) / (float)dim;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int n = chunk_values(gl + i * lanes, dim);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) { v[i][j] = j < n ? v[i][j] - mean : 0.f; s += v[i][j] * v[i][j]; }
+    }
+    const float rstd = 1.f / sqrtf(sum.one(s) / (float)dim + a.eps);
+    if (gl == 0) {
+        if (a.mean) a.mean[row] = mean;
+        if (a.rstd) a.rstd[row] = rstd;
+    }
+    TY *y = static_cast<TY *>(a.y) + row * a.ldy;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = gl + i * lanes, n = chunk_values(c, dim);
+        f32x8 h;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[j] = v[i][j] * rstd;
+        if (a.q && c * CHUNK < a.s.pitch) pack_chunk(a.q + row * a.s.pitch, a.e + row * (a.s.pitch / PACK_BLOCK), c, h);
+        if (n <= 0) continue;
+        const f32x8 g = a.gamma ? load_some(a.gamma + c * CHUNK, n) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
+        const f32x8 b = a.beta ? load_some(a.beta + c * CHUNK, n) : f32x8{};
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[j] = h[j] * g[j] + b[j];
+        store_some(y + c * CHUNK, h, n);
+    }
+}
+
+// Backward: with n the normalised row and g = dy gamma, dx = rstd (g - mean(g) - n mean(g n)) + residual; dgamma = sum over rows of
+// dy n, dbeta of dy.  A workgroup goes through rows in steps of the grid and keeps its columns' sums in registers; what it has summed goes
+// to `partial` ([workgroup][dgamma, dbeta][width rounded up to a chunk]), and column_sum_kernel adds that up in the order of the
+// workgroups: the same bits every time.
+struct NormBackArgs {
+    const void *dy, *x;
+    const float *mean, *rstd;
+    const int8_t *q;        // normalised rows in 8 bits; null: from x, mean and rstd
+    const uint8_t *e;
+    const float *gamma;
+    const void *residual;   // added to dx, or null
+    void *dx;
+    float *partial;
+    int64_t lddy, ldx, ldr, lddx, rows;
+    RowShape s;
+};
+
+template <typename TX, typename TY, int NV, bool BLOCK>
+__global__ __launch_bounds__(BLOCK ? 1024 : ROW_THREADS) void norm_back_kernel(NormBackArgs a)
+{
+    extern __shared__ float cols[];                // [2][width], where several rows' lanes share columns
+    __shared__ float lds[64];
+    const int lanes = a.s.lanes, gl = threadIdx.x % lanes, dim = a.s.dim;
+    const int64_t per = BLOCK ? 1 : ROW_THREADS / lanes, step = per * gridDim.x;
+    RowSum<BLOCK> sum(lds, lanes);
+    f32x8 dg[NV], db[NV], gamma[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int c = gl + i * lanes, n = chunk_values(c, dim);
+        dg[i] = db[i] = f32x8{};
+        gamma[i] = n <= 0 ? f32x8{} : a.gamma ? load_some(a.gamma + c * CHUNK, n) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
+    }
+    for (int64_t row = (int64_t)blockIdx.x * per + (BLOCK ? 0 : threadIdx.x / lanes); row < a.rows; row += step) {
+        const TY *dy = static_cast<const TY *>(a.dy) + row * a.lddy;
+        f32x8 d[NV], h[NV];
+        const float rstd = a.rstd[row], mean = a.q ? 0.f : a.mean[row];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = gl + i * lanes, n = chunk_values(c, dim);
+            d[i] = n > 0 ? load_some(dy + c * CHUNK, n) : f32x8{};
+            h[i] = f32x8{};
+            if (n <= 0) continue;
+            if (a.q) {
+                uint64_t q;
+                __builtin_memcpy(&q, a.q + row * a.s.pitch + c * CHUNK, 8);
+                h[i] = unpack_chunk(q, a.e[row * (a.s.pitch / PACK_BLOCK) + (c >> 2)]);
+            } else {
+                h[i] = load_some(static_cast<const TX *>(a.x) + row * a.ldx + c * CHUNK, n);
+            }
+        }
+        float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int n = chunk_values(gl + i * lanes, dim);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (!a.q) h[i][j] = (h[i][j] - mean) * rstd;
+                if (j >= n) { h[i][j] = 0.f; d[i][j] = 0.f; }
+                dg[i][j] += d[i][j] * h[i][j];
+                db[i][j] += d[i][j];
+                d[i][j] *= gamma[i][j];
+                s1 += d[i][j];
+                s2 += d[i][j] * h[i][j];
+            }
+        }
+        sum.two(s1, s2);
+        s1 /= (float)dim; s2 /= (float)dim;
+        TX *dx = static_cast<TX *>(a.dx) + row * a.lddx;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = gl + i * lanes, n = chunk_values(c, dim);
+            if (n <= 0) continue;
+            f32x8 o;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] = rstd * (d[i][j] - s1 - h[i][j] * s2);
+            if (a.residual) {
+                const f32x8 r = load_some(static_cast<const TX *>(a.residual) + row * a.ldr + c * CHUNK, n);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] += r[j];
+            }
+            store_some(dx + c * CHUNK, o, n);
+        }
+    }
+    const int width = (dim + CHUNK - 1) / CHUNK * CHUNK;
+    float *out = a.partial + (size_t)blockIdx.x * 2 * width;
+    if (BLOCK) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = gl + i * lanes;
+            if (c * CHUNK >= width) continue;
+            store_chunk(out + c * CHUNK, dg[i]);
+            store_chunk(out + width + c * CHUNK, db[i]);
+        }
+        return;
+    }
+    // lanes of a wave that hold the same columns of other rows, then the waves one after the other
+    for (int o = lanes; o < 64; o <<= 1)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { dg[i][j] += __shfl_xor(dg[i][j], o); db[i][j] += __shfl_xor(db[i][j], o); }
+    for (int w = 0; w < ROW_WAVES; ++w) {
+        if ((int)threadIdx.x / 64 == w && (int)threadIdx.x % 64 < lanes)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int c = gl + i * lanes;
+                if (c * CHUNK >= width) continue;
+                float *p = cols + c * CHUNK, *r = cols + width + c * CHUNK;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) { p[j] = w ? p[j] + dg[i][j] : dg[i][j]; r[j] = w ? r[j] + db[i][j] : db[i][j]; }
+            }
+        __syncthreads();
+    }
+    for (int c = threadIdx.x; c < 2 * width; c += ROW_THREADS) out[c] = cols[c];
+}
+
+// Column sums of partial[n][sets][width]: set s goes to out[s] (null: nobody asks).  16 columns a workgroup, 16 threads for each of them, which
+// take every 16th row; their sums are added in order.
+struct ColumnSumArgs {
+    const float *partial;
+    float *out[2];
+    int n, sets, width, dim;
+};
+
+static __global__ __launch_bounds__(256) void column_sum_kernel(ColumnSumArgs a)
+{
+    __shared__ float lds[16][17];
+    const int cx = threadIdx.x % 16, ry = threadIdx.x / 16, col = blockIdx.x * 16 + cx, total = a.sets * a.width;
+    float s = 0.f;
+    if (col < total) {
+        const float *p = a.partial + col;
+        int r = ry;
+        for (; r + 7 * 16 < a.n; r += 8 * 16) {
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = p[(size_t)(r + u * 16) * total];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += v[u];
+        }
+        for (; r < a.n; r += 16) s += p[(size_t)r * total];
+    }
+    lds[ry][cx] = s;
+    __syncthreads();
+    if (ry || col >= total) return;
+#pragma unroll
+    for (int u = 1; u < 16; ++u) s += lds[u][cx];
+    const int set = col / a.width, at = col % a.width;
+    if (at < a.dim && a.out[set]) a.out[set][at] = s;
+}
+
+// ---- the slope of the activation and the bias' gradient -------------------------------------------------
+// dz = dy act'(z), handed on in the layer's type (the matrix instructions take it so); dbias = column sums of dz before that rounding.
+// A thread holds 8 columns and goes down the rows; 32 of them side by side, 8 below each other, and the partial sums as above.
+struct SlopeArgs {
+    const void *dy, *z;
+    const int8_t *q;         // z in 8 bits; null: z, or no activation
+    const uint8_t *e;
+    void *dz;
+    float *partial;          // null: no bias
+    int64_t lddy, ldz, lddz, rows;
+    int dim, pitch, act;
+};
+
+constexpr int SLOPE_COLS = 32 * CHUNK;
+
+template <typename T, typename TY>
+__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
+{
+    __shared__ float lds[8][SLOPE_COLS];
+    const int cx = threadIdx.x % 32, ry = threadIdx.x / 32, c = blockIdx.x * 32 + cx, n = chunk_values(c, a.dim);
+    f32x8 s = {};
+    if (n > 0)
+        for (int64_t row = (int64_t)blockIdx.y * 8 + ry; row < a.rows; row += 8 * (int64_t)gridDim.y) {
+            f32x8 d = load_some(static_cast<const TY *>(a.dy) + row * a.lddy + c * CHUNK, n);
+            if (a.act != DENSE_ACT_NONE) {
+                f32x8 z;
+                if (a.q) {
+                    uint64_t q;
+                    __builtin_memcpy(&q, a.q + row * a.pitch + c * CHUNK, 8);
+                    z = unpack_chunk(q, a.e[row * (a.pitch / PACK_BLOCK) + (c >> 2)]);
+                } else {
+                    z = load_some(static_cast<const T *>(a.z) + row * a.ldz + c * CHUNK, n);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[j] *= act_slope(a.act, z[j]);
+            }
+            if (a.dz) store_some(static_cast<T *>(a.dz) + row * a.lddz + c * CHUNK, d, n);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] += j < n ? d[j] : 0.f;
+        }
+    if (!a.partial) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) lds[ry][cx * CHUNK + j] = s[j];
+    __syncthreads();
+    const int col = blockIdx.x * SLOPE_COLS + threadIdx.x, width = (a.dim + CHUNK - 1) / CHUNK * CHUNK;
+    if (col >= width) return;
+    float t = lds[0][threadIdx.x];
+#pragma unroll
+    for (int u = 1; u < 8; ++u) t += lds[u][threadIdx.x];
+    a.partial[(size_t)blockIdx.y * width + col] = t;
+}
+
+// ---- to 8 bits and back -------------------------------------------------------------------------------
+struct PackArgs {
+    const void *x;
+    int8_t *q;
+    uint8_t *e;
+    int64_t ldx, rows;
+    int dim, pitch;
+};
+
+// One chunk a thread; the four lanes of a block lie in one wave (the pitch is whole blocks).
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(PackArgs a)
+{
+    const int per = a.pitch / CHUNK;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+    if (row >= a.rows) return;                      // (whole blocks: a row has four lanes or a multiple)
+    const int c = (int)(i - row * per), n = chunk_values(c, a.dim);
+    const f32x8 v = n > 0 ? load_some(static_cast<const T *>(a.x) + row * a.ldx + c * CHUNK, n) : f32x8{};
+    pack_chunk(a.q + row * a.pitch, a.e + row * (a.pitch / PACK_BLOCK), c, v);
+}
+
+// y = act(gamma v + beta) of the values v that q and e stand for.
+struct ExpandArgs {
+    const int8_t *q;
+    const uint8_t *e;
+    const float *gamma, *beta;
+    void *y;
+    int64_t ldy, rows;
+    int dim, pitch, act;
+};
+
+// A value that fits the 8-bit form may lie above fp16's largest number by the rounding to whole steps alone (65536 for 65504): it is that number.
+template <typename T> __device__ __forceinline__ float within(float v) { return v; }
+template <> __device__ __forceinline__ float within<f16>(float v)
+{
+    return v >= 65520.f && v <= 65536.f ? 65504.f : v <= -65520.f && v >= -65536.f ? -65504.f : v;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void expand_kernel(ExpandArgs a)
+{
+    const int per = (a.dim + CHUNK - 1) / CHUNK;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+    if (row >= a.rows) return;
+    const int c = (int)(i - row * per), n = chunk_values(c, a.dim);
+    uint64_t q;
+    __builtin_memcpy(&q, a.q + row * a.pitch + c * CHUNK, 8);
+    f32x8 v = unpack_chunk(q, a.e[row * (a.pitch / PACK_BLOCK) + (c >> 2)]);
+    if (a.gamma) {
+        const f32x8 g = load_some(a.gamma + c * CHUNK, n);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= g[j];
+    }
+    if (a.beta) {
+        const f32x8 b = load_some(a.beta + c * CHUNK, n);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += b[j];
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = within<T>(act_value(a.act, v[j]));
+    store_some(static_cast<T *>(a.y) + row * a.ldy + c * CHUNK, v, n);
+}
+
+} // namespace het

@@ -1,0 +1,165 @@
+// What the dense layers' kernels share: element types, pieces of 16 bytes and less at any alignment, activations and the 8-bit form of
+// activations (gfx950, wave64).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace het {
+
+using bf16 = __bf16;
+using f16 = _Float16;
+
+template <typename T, int N> using vec = T __attribute__((ext_vector_type(N)));
+
+using f32x4 = vec<float, 4>;
+using f32x8 = vec<float, 8>;
+using f32x16 = vec<float, 16>;
+using i32x4 = vec<int32_t, 4>;
+
+constexpr int CHUNK = 8;             // elements a lane handles at a time in the row-wise kernels
+constexpr int PACK_BLOCK = 32;       // values that share a step in the 8-bit form
+constexpr uint32_t PACK_NOT_FINITE = 255;
+
+// ---- pieces of rows at any alignment ------------------------------------------------------------------
+// Rows may begin at any element (odd widths, wider matrices), and the vector memory path takes any address: a piece is one load
+// of 16 bytes (two for fp32) whatever its alignment, and no second set of kernels is needed for odd strides.
+
+template <typename T>
+__device__ __forceinline__ f32x8 load_chunk(const T *p)
+{
+    vec<T, 8> v;
+    __builtin_memcpy(&v, p, sizeof(v));
+    return __builtin_convertvector(v, f32x8);
+}
+
+template <typename T>
+__device__ __forceinline__ void store_chunk(T *p, f32x8 f)
+{
+    const vec<T, 8> v = __builtin_convertvector(f, vec<T, 8>);
+    __builtin_memcpy(p, &v, sizeof(v));
+}
+
+// The first `n` (0 .. 8) of a chunk; the others read as zero and are not written.
+template <typename T>
+__device__ __forceinline__ f32x8 load_some(const T *p, int n)
+{
+    if (n >= CHUNK) return load_chunk(p);
+    f32x8 f = {};
+#pragma unroll
+    for (int j = 0; j < CHUNK - 1; ++j) if (j < n) f[j] = (float)p[j];
+    return f;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_some(T *p, f32x8 f, int n)
+{
+    if (n >= CHUNK) { store_chunk(p, f); return; }
+#pragma unroll
+    for (int j = 0; j < CHUNK - 1; ++j) if (j < n) p[j] = (T)f[j];
+}
+
+// ---- activations --------------------------------------------------------------------------------------
+enum { DENSE_ACT_NONE = 0, DENSE_ACT_RELU = 1, DENSE_ACT_GELU = 2, DENSE_ACT_SILU = 3 };
+
+__device__ __forceinline__ float act_value(int act, float v)
+{
+    switch (act) {
+    case DENSE_ACT_RELU: return v > 0.f ? v : v == v ? 0.f : v;                       // NaN stays NaN
+    case DENSE_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+    case DENSE_ACT_SILU: return v / (1.f + expf(-v));
+    default: return v;
+    }
+}
+
+__device__ __forceinline__ float act_slope(int act, float v)
+{
+    switch (act) {
+    case DENSE_ACT_RELU: return v > 0.f ? 1.f : v == v ? 0.f : v;
+    case DENSE_ACT_GELU: return 0.5f * (1.f + erff(v * 0.70710678118654752f)) + v * (0.39894228040143268f * expf(-0.5f * v * v));
+    case DENSE_ACT_SILU: { const float p = 1.f / (1.f + expf(-v)); return p * (1.f + v * (1.f - p)); }
+    default: return 1.f;
+    }
+}
+
+// ---- the 8-bit form -----------------------------------------------------------------------------------
+// A block of 32 values along a row shares a step 2^e; a value is q steps, q whole in [-127, 127] (ties to even).  e is the smallest
+// for which the block's largest magnitude rounds to at most 127 steps, so a value is off by at most half a step, 1/127 of that
+// magnitude.  The step is a power of two because q 2^e then fits bf16's 8 significant bits: the matrix instructions of the backward
+// pass take exactly what was kept.  e is held as the byte e + 127, the exponent field of the float 2^e.  A block with an infinity or a
+// NaN has the byte 255 and reads as NaN everywhere: what overflowed is not taken for a number later on.
+
+// Largest magnitude as the bits of a float: as whole numbers they are in the order of the magnitudes, with NaN above infinity.
+__device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+struct PackStep {
+    uint32_t byte;       // what is stored
+    float inverse;       // 2^-e
+    float most;          // largest number of steps
+};
+
+// most_bits: magnitude() of the block's largest value.  A significand of 127.5 / 64 and above rounds to 128 steps: adding 2^16 (its distance
+// from 2) carries into the exponent exactly then.
+__device__ __forceinline__ PackStep pack_step(uint32_t most_bits)
+{
+    PackStep s;
+    int e = (int)((most_bits + 0x10000u) >> 23) - 133;
+    e = e < -126 ? -126 : e > 122 ? 122 : e;
+    s.byte = most_bits >= 0x7F800000u ? PACK_NOT_FINITE : (uint32_t)(e + 127);
+    s.inverse = most_bits >= 0x7F800000u ? 0.f : __uint_as_float((uint32_t)(127 - e) << 23);
+    s.most = e == 122 ? 63.f : 127.f;       // 64 steps of 2^122 would be no float any more
+    return s;
+}
+
+__device__ __forceinline__ int pack_value(float v, const PackStep &s)
+{
+    if (s.byte == PACK_NOT_FINITE) return 0;
+    const float q = __builtin_rintf(v * s.inverse);
+    return (int)(q > s.most ? s.most : q < -s.most ? -s.most : q);
+}
+
+__device__ __forceinline__ uint32_t pack_four(float a, float b, float c, float d, const PackStep &s)
+{
+    return ((uint32_t)pack_value(a, s) & 255u) | ((uint32_t)pack_value(b, s) & 255u) << 8 | ((uint32_t)pack_value(c, s) & 255u) << 16 |
+           (uint32_t)pack_value(d, s) << 24;
+}
+
+// 2^e of a stored byte; 255 gives infinity, and 0 times that the NaN the block stands for.
+__device__ __forceinline__ float pack_step_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+__device__ __forceinline__ f32x8 unpack_chunk(uint64_t q, uint32_t byte)
+{
+    const float step = pack_step_of(byte);
+    f32x8 f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = (float)(int8_t)(q >> (8 * j)) * step;
+    return f;
+}
+
+// The magnitude over the four lanes (aligned) that hold a block of 32 values, eight each.
+__device__ __forceinline__ uint32_t quad_max(uint32_t v)
+{
+    uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xf, 0xf, false);       // lanes 1 0 3 2
+    v = v > o ? v : o;
+    o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xf, 0xf, false);                // lanes 2 3 0 1
+    return v > o ? v : o;
+}
+
+__device__ __forceinline__ uint32_t chunk_magnitude(f32x8 f)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) { const uint32_t b = magnitude(f[j]); m = m > b ? m : b; }
+    return m;
+}
+
+// Writes this lane's chunk of a row's 8-bit form and, by the first of a block's four lanes, the block's step.  All four lanes are active; values
+// behind the row's end come as zero.
+__device__ __forceinline__ void pack_chunk(int8_t *q, uint8_t *e, int c, f32x8 f)
+{
+    const PackStep s = pack_step(quad_max(chunk_magnitude(f)));
+    const uint2 w = {pack_four(f[0], f[1], f[2], f[3], s), pack_four(f[4], f[5], f[6], f[7], s)};
+    *reinterpret_cast<uint2 *>(q + (size_t)c * CHUNK) = w;
+    if ((c & 3) == 0) e[c >> 2] = (uint8_t)s.byte;
+}
+
+} // namespace het
