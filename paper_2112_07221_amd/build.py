@@ -11,7 +11,7 @@ from concurrent.futures import ThreadPoolExecutor
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 # (source, parts it is compiled in): the parts run side by side; the sources check that they are as many as they have
-SOURCES = [("het_cache.hip", 1), ("apply_variants.hip", 8), ("fill_variants.hip", 2), ("dense.hip", 1), ("dense_product.hip", 3)]
+SOURCES = [("het_cache.hip", 1), ("apply_variants.hip", 8), ("fill_variants.hip", 2), ("dense.hip", 1), ("dense_norm.hip", 5), ("dense_product.hip", 3)]
 OUT = os.path.join(HERE, "libhet_cache.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

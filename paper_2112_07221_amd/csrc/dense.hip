@@ -32,53 +32,7 @@ int launched()
     return HET_EHIP;
 }
 
-struct Shape { RowShape s; int nv; bool block; };
-
-// Where a row of `dim` values lies (see RowShape).
-Shape shape_of(int dim)
-{
-    Shape h;
-    const int chunks = (int)cdiv(dim, CHUNK);
-    h.s.dim = dim; h.s.pitch = pitch_of(dim);
-    h.block = dim > ROW_WIDE;
-    if (h.block) {
-        h.s.lanes = dim <= 256 * CHUNK * 4 ? 256 : dim <= 512 * CHUNK * 4 ? 512 : 1024;
-    } else {
-        h.s.lanes = 4;
-        while (h.s.lanes < 64 && h.s.lanes < chunks) h.s.lanes *= 2;
-    }
-    const int n = (int)cdiv(chunks, h.s.lanes);
-    h.nv = n <= 1 ? 1 : n <= 2 ? 2 : 4;
-    return h;
-}
-
-int rows_per_group(const Shape &h) { return h.block ? 1 : ROW_THREADS / h.s.lanes; }
-
-int norm_groups(int64_t rows, const Shape &h) { return (int)std::min<int64_t>(PARTIALS, cdiv(rows, rows_per_group(h))); }
-
-template <typename TX, typename TY>
-void launch_norm(const NormArgs &a, const Shape &h, hipStream_t st)
-{
-    const dim3 grid((uint32_t)cdiv(a.rows, rows_per_group(h)));
-    if (h.block) {
-        if (h.nv == 2) norm_kernel<TX, TY, 2, true><<<grid, h.s.lanes, 0, st>>>(a);
-        else norm_kernel<TX, TY, 4, true><<<grid, h.s.lanes, 0, st>>>(a);
-    } else if (h.nv == 1) norm_kernel<TX, TY, 1, false><<<grid, ROW_THREADS, 0, st>>>(a);
-    else if (h.nv == 2) norm_kernel<TX, TY, 2, false><<<grid, ROW_THREADS, 0, st>>>(a);
-    else norm_kernel<TX, TY, 4, false><<<grid, ROW_THREADS, 0, st>>>(a);
-}
-
-template <typename TX, typename TY>
-void launch_norm_back(const NormBackArgs &a, const Shape &h, int groups, hipStream_t st)
-{
-    const size_t lds = h.block ? 0 : 2 * (size_t)width_of(h.s.dim) * sizeof(float);
-    if (h.block) {
-        if (h.nv == 2) norm_back_kernel<TX, TY, 2, true><<<groups, h.s.lanes, lds, st>>>(a);
-        else norm_back_kernel<TX, TY, 4, true><<<groups, h.s.lanes, lds, st>>>(a);
-    } else if (h.nv == 1) norm_back_kernel<TX, TY, 1, false><<<groups, ROW_THREADS, lds, st>>>(a);
-    else if (h.nv == 2) norm_back_kernel<TX, TY, 2, false><<<groups, ROW_THREADS, lds, st>>>(a);
-    else norm_back_kernel<TX, TY, 4, false><<<groups, ROW_THREADS, lds, st>>>(a);
-}
+int norm_groups(int64_t rows, const NormShape &h) { return (int)std::min<int64_t>(PARTIALS, cdiv(rows, h.rows)); }
 
 void launch_column_sum(const float *partial, int n, int sets, int dim, float *out0, float *out1, hipStream_t st)
 {
@@ -123,6 +77,13 @@ bool linear_sizes(const het_linear_t *l)
            l->rows * std::max(l->in, l->out) <= MOST_VALUES;
 }
 
+template <typename T, typename TY>
+void launch_slope(const SlopeArgs &s, dim3 grid, hipStream_t st)
+{
+    if (s.dim % CHUNK == 0) slope_kernel<T, TY, true><<<grid, 256, 0, st>>>(s);
+    else slope_kernel<T, TY, false><<<grid, 256, 0, st>>>(s);
+}
+
 int slope_splits(int64_t rows, int32_t out)
 {
     // enough workgroups to fill the chip, at least 32 rows for each
@@ -160,7 +121,7 @@ int het_layer_norm(const void *x, int32_t x_type, int64_t ldx, const float *gamm
     if (!norm_sizes(rows, dim) || !known_pair(x_type, y_type) || !(eps >= 0.f) || ldx < dim || ldy < dim || !q != !e) return HET_EINVAL;
     if (rows == 0) return HET_OK;
     if (!x || !y || !aligned16(q)) return HET_EINVAL;
-    const Shape h = shape_of(dim);
+    const NormShape h = norm_shape(dim);
     NormArgs a{x, gamma, beta, y, mean, rstd, q, e, ldx, ldy, rows, h.s, eps};
     with_types(x_type, y_type, [&](auto tx, auto ty) {
         launch_norm<typename decltype(tx)::type, typename decltype(ty)::type>(a, h, static_cast<hipStream_t>(hip_stream));
@@ -171,7 +132,7 @@ int het_layer_norm(const void *x, int32_t x_type, int64_t ldx, const float *gamm
 int64_t het_layer_norm_workspace(int64_t rows, int32_t dim)
 {
     if (!norm_sizes(rows, dim)) return HET_EINVAL;
-    return (int64_t)norm_groups(rows, shape_of(dim)) * 2 * width_of(dim) * 4;
+    return (int64_t)norm_groups(rows, norm_shape(dim)) * 2 * width_of(dim) * 4;
 }
 
 int het_layer_norm_backward(const void *dy, int32_t y_type, int64_t lddy, const void *x, int32_t x_type, int64_t ldx,
@@ -185,12 +146,14 @@ int het_layer_norm_backward(const void *dy, int32_t y_type, int64_t lddy, const 
     if (rows > 0 && (!dy || !dx || !rstd || (!q && (!x || !mean)) || !aligned16(q))) return HET_EINVAL;
     if (!workspace_ok(workspace, workspace_bytes, het_layer_norm_workspace(rows, dim))) return HET_EINVAL;
     if (rows == 0 && !dgamma && !dbeta) return HET_OK;
-    const Shape h = shape_of(dim);
+    const NormShape h = norm_shape(dim);
     const int groups = norm_groups(rows, h);
     float *partial = static_cast<float *>(workspace);
     if (rows > 0) {
         NormBackArgs a{dy, x, mean, rstd, q, e, gamma, residual, dx, partial, lddy, ldx, ld_residual, lddx, rows, h.s};
-        with_types(x_type, y_type, [&](auto tx, auto ty) { launch_norm_back<typename decltype(tx)::type, typename decltype(ty)::type>(a, h, groups, st); });
+        with_types(x_type, y_type, [&](auto tx, auto ty) {
+            launch_norm_back<typename decltype(tx)::type, typename decltype(ty)::type>(a, h, groups, st);
+        });
     }
     if (dgamma || dbeta) launch_column_sum(partial, groups, 2, dim, dgamma, dbeta, st);
     return launched();
@@ -275,7 +238,7 @@ int het_linear_backward(const het_linear_t *l, void *hip_stream)
         s.partial = l->dbias ? reinterpret_cast<float *>(ws + p.bias_at) : nullptr;
         s.rows = l->rows; s.dim = l->out; s.pitch = pitch_of(l->out); s.act = l->act;
         const dim3 grid((uint32_t)cdiv(l->out, SLOPE_COLS), (uint32_t)p.slope);
-        with_types(l->y_type, l->type, [&](auto ty, auto t) { slope_kernel<typename decltype(t)::type, typename decltype(ty)::type><<<grid, 256, 0, st>>>(s); });
+        with_types(l->y_type, l->type, [&](auto ty, auto t) { launch_slope<typename decltype(t)::type, typename decltype(ty)::type>(s, grid, st); });
         if (l->dbias) launch_column_sum(s.partial, p.slope, 1, l->out, l->dbias, nullptr, st);
     }
     const void *dz = dz_is_dy ? l->dy : l->dz;

@@ -1,13 +1,15 @@
-// Which kernel a product takes, and its launch (dense_product.hip).
+// Which kernel a call takes, and its launch (dense_product.hip, dense_norm.hip).
 #pragma once
 #include "dense_product.hpp"
+#include "dense_rows.hpp"
 
 namespace het {
 
 struct ProductPlan {
     bool ok;                    // the grid fits
-    int few;                    // 16-row tiles of the kernel for few rows; 0: tiles of product_any_kernel
-    int m, n, k, tiles_m, tiles_n, splits, k_split;
+    int few;                    // 16-row tiles of the kernel for few rows; 0: another kernel
+    int tile;                   // edge of product_kernel's tile
+    int m, n, k, splits, k_split;
     int64_t partial_bytes;
 };
 
@@ -16,5 +18,16 @@ ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bo
 
 // Fills in the sizes of `a` and enqueues the product.
 void launch_product(ProductArgs a, const ProductPlan &p, int type, bool a_k, bool b_k, hipStream_t st);
+
+// How layer norm's rows lie: RowShape, rows a workgroup holds at a time, chunks a lane.
+struct NormShape {
+    RowShape s;
+    int rows, nv;
+    bool block;
+};
+
+NormShape norm_shape(int dim);
+template <typename TX, typename TY> void launch_norm(const NormArgs &a, const NormShape &h, hipStream_t st);
+template <typename TX, typename TY> void launch_norm_back(const NormBackArgs &a, const NormShape &h, int groups, hipStream_t st);
 
 } // namespace het

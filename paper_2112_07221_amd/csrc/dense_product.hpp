@@ -60,9 +60,7 @@ __device__ __forceinline__ void finish_value(const Finish &f, int64_t row, int c
 {
     if (n <= 0) return;
     if (f.z) store_some(static_cast<T *>(f.z) + row * f.ldz + col, v, n);
-    if (f.act != DENSE_ACT_NONE)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = act_value(f.act, v[j]);
+    v = act_chunk<false>(f.act, v);
     if (f.y_f32) finish_store<float>(f, row, col, n, v);
     else finish_store<T>(f, row, col, n, v);
 }
@@ -112,7 +110,7 @@ struct Tile {
 
     __device__ static __forceinline__ int mixed(int r, int c)     // place of piece c of row (or k) r
     {
-        if (K) return r * 8 + (c ^ (PERMUTED ? (r & 3) | ((r >> 2) & 4) : r & 7));
+        if (K) return r * 8 + (c ^ (PERMUTED ? (r >> 1 & 3) | (r >> 2 & 4) : r >> 1 & 7));
         if (sizeof(T) == 2) return r * WIDE + (c ^ (4 * (r & 3)));
         return r * WIDE + (c ^ (8 * ((r >> 2) & 1)));
     }
@@ -181,44 +179,213 @@ __device__ __forceinline__ int tile_of(int block, int tiles)
 // Tiles in bands of 8 rows of tiles: neighbours share A's rows or B's.
 __device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int &tm, int &tn)
 {
-    const int band = t / (8 * tiles_n), first = band * 8, high = tiles_m - first < 8 ? tiles_m - first : 8, in = t - band * 8 * tiles_n;
+    const int band = t / (8 * tiles_n), first = band * 8, high = tiles_m - first < 8 ? tiles_m - first  : 8, in = t - band * 8 * tiles_n;
     tm = first + in % high;
     tn = in / high;
 }
 
-// Ends a wave's 32 x 32 sums at (row0, col0): 16 columns a lane.
-template <typename T>
-__device__ __forceinline__ void finish_tile(const ProductArgs &a, int split, int row0, int col0, const f32x16 &acc)
+// Four chunks at `col` of the rows row, row + 8, ...; sums(r): the chunk of row r of the 32.
+template <typename T, typename TY, typename S>
+__device__ __forceinline__ void finish_whole(const Finish &f, int64_t row, int col, S &&sums)
 {
-    const int lane = threadIdx.x % 64, row = row0 + lane % 32, col = col0 + 16 * (lane / 32);
-    if (row >= a.m || col0 >= a.n) return;
-    f32x8 v[2];
+    const int first = threadIdx.x % 64 / 8;
+    vec<TY, 8> res[4];
+    if (f.residual)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) { v[0][j] = acc[j]; v[1][j] = acc[8 + j]; }
+        for (int it = 0; it < 4; ++it) __builtin_memcpy(&res[it], static_cast<const TY *>(f.residual) + (row + 8 * it) * f.ldr + col, sizeof(res[it]));
+    const f32x8 bias = f.bias ? load_chunk(f.bias + col) : f32x8{};
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int64_t at = row + 8 * it;
+        f32x8 v = sums(first + 8 * it);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += bias[j];
+        if (f.q) pack_chunk(f.q + at * f.pitch, f.e + at * (f.pitch / PACK_BLOCK), col / CHUNK, v);
+        if (f.z) store_chunk(static_cast<T *>(f.z) + at * f.ldz + col, v);
+        v = act_chunk<false>(f.act, v);
+        if (f.residual)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += (float)res[it][j];
+        store_chunk(static_cast<TY *>(f.y) + at * f.ldy + col, v);
+    }
+}
+
+// Ends a wave's 32 x 64 sums at (row0, col0).  They go through the wave's own 8 KB of LDS (the tiles' are free by then), so that eight lanes
+// hold a row's 64 columns side by side: whole 128-byte pieces of rows are stored, four lanes share a block of the 8-bit form, and the
+// code is there once for all of a lane's sums.
+constexpr int FINISH_PIECES = 32 * 64 / 4;
+
+template <typename T>
+__device__ __forceinline__ void finish_tile(const ProductArgs &a, int split, int row0, int col0, const f32x16 &left, const f32x16 &right, f32x4 *lds)
+{
+    const int lane = threadIdx.x % 64;
+    {
+        const int r = lane % 32, h = lane / 32;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");        // the lanes' reads of what was there before
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            lds[r * 16 + ((4 * h + q) ^ (r & 7))] = f32x4{left[4 * q], left[4 * q + 1], left[4 * q + 2], left[4 * q + 3]};
+            lds[r * 16 + ((8 + 4 * h + q) ^ (r & 7))] = f32x4{right[4 * q], right[4 * q + 1], right[4 * q + 2], right[4 * q + 3]};
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+    const int c = lane % 8, col = col0 + c * CHUNK;
+    auto sums = [&](int r) {
+        const f32x4 lo = lds[r * 16 + ((2 * c) ^ (r & 7))], hi = lds[r * 16 + ((2 * c + 1) ^ (r & 7))];
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
     if (a.splits > 1) {
         const int width = partial_width(a.n);
-        if (col >= width) return;
-        float *p = a.partial + ((int64_t)split * a.m + row) * width + col;
-        store_chunk(p, v[0]);
-        store_chunk(p + 8, v[1]);
-        return;
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const int r = 8 * it + lane / 8, row = row0 + r;
+            if (col < width && row < a.m) store_chunk(a.partial + ((int64_t)split * a.m + row) * width + col, sums(r));
+        }
+    } else if (row0 + 32 <= a.m && col0 + 64 <= a.n) {                 // all of it in the matrix: no edge is looked for, four rows' residuals are under way
+        if (a.f.y_f32) finish_whole<T, float>(a.f, row0 + lane / 8, col, sums);
+        else finish_whole<T, T>(a.f, row0 + lane / 8, col, sums);
+    } else if (col0 + (c & ~3) * CHUNK < a.n) {                        // (a block's four lanes go together)
+#pragma unroll 1
+        for (int it = 0; it < 4; ++it) {
+            const int r = 8 * it + lane / 8, row = row0 + r, n = a.n - col;
+            if (row >= a.m) return;
+            const f32x8 v = finish_bias(a.f, col, n, sums(r));
+            if (a.f.q) pack_chunk(a.f.q + (int64_t)row * a.f.pitch, a.f.e + (int64_t)row * (a.f.pitch / PACK_BLOCK), col / CHUNK, v);
+            finish_value<T>(a.f, row, col, n, v);
+        }
     }
-    v[0] = finish_bias(a.f, col, a.n - col, v[0]);
-    v[1] = finish_bias(a.f, col + 8, a.n - col - 8, v[1]);
-    if (a.f.q) {
-        uint32_t most = chunk_magnitude(v[0]);
-        const uint32_t o = chunk_magnitude(v[1]);
-        most = most > o ? most : o;
-        const uint32_t other = __shfl_xor(most, 32);
-        const PackStep s = pack_step(most > other ? most : other);
-        uint4 w;
-        w.x = pack_four(v[0][0], v[0][1], v[0][2], v[0][3], s); w.y = pack_four(v[0][4], v[0][5], v[0][6], v[0][7], s);
-        w.z = pack_four(v[1][0], v[1][1], v[1][2], v[1][3], s); w.w = pack_four(v[1][4], v[1][5], v[1][6], v[1][7], s);
-        *reinterpret_cast<uint4 *>(a.f.q + (int64_t)row * a.f.pitch + col) = w;
-        if (lane < 32) a.f.e[(int64_t)row * (a.f.pitch / PACK_BLOCK) + col0 / PACK_BLOCK] = (uint8_t)s.byte;
+}
+
+// The wave's part of two tiles' LDS.
+template <int WAVES>
+__device__ __forceinline__ f32x4 *finish_room(i32x4 *first, i32x4 *second)
+{
+    const int wave = threadIdx.x / 64;
+    return reinterpret_cast<f32x4 *>(wave < WAVES / 2 ? first : second) + wave % (WAVES / 2) * FINISH_PIECES;
+}
+
+// ---- aligned operands -------------------------------------------------------------------------------------
+// TM x TN tiles, WM x WN waves.  Memory goes straight to LDS, 16 bytes a lane, one step ahead of the products: the next step's pieces are on their way
+// while a step is multiplied, and nothing passes through registers.  Pieces behind an edge are asked for outside the buffer's range, which
+// reads as zero.  Operands' rows begin at multiples of 16 bytes and their widths are whole pieces (the host looks).
+__device__ __forceinline__ void copies_done() { __builtin_amdgcn_s_waitcnt(0x0F70); }        // vmcnt(0) alone
+
+template <typename T, int R, bool K, bool PERMUTED, int THREADS>
+struct Copy : Tile<T, R, K, PERMUTED> {
+    using B = Tile<T, R, K, PERMUTED>;
+    static constexpr int EACH = B::PIECES / THREADS;
+    static constexpr int OUTSIDE = (int)0x80000000;
+    int at[EACH];               // byte offsets of this thread's pieces from the tile's corner; OUTSIDE: behind the matrix' last row
+    int64_t advance;            // bytes from a step to the next
+    const char *corner;
+
+    // row0: the tile's first row; k0: the first k.
+    __device__ __forceinline__ Copy(const T *p, int64_t ld, int row0, int rows, int k0)
+    {
+        corner = reinterpret_cast<const char *>(p + (K ? (int64_t)row0 * ld + k0 : (int64_t)k0 * ld + row0));
+        advance = (K ? (int64_t)B::STEP : B::STEP * ld) * (int64_t)sizeof(T);
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+            const int i = u * THREADS + threadIdx.x, down = i / B::WIDE, along = along_of(i);
+            const int row = K ? down : along * B::PIECE;
+            at[u] = row0 + row < rows ? (int)((down * ld + along * B::PIECE) * (int64_t)sizeof(T)) : OUTSIDE;
+        }
     }
-    finish_value<T>(a.f, row, col, a.n - col, v[0]);
-    finish_value<T>(a.f, row, col + 8, a.n - col - 8, v[1]);
+    // The piece that belongs at place i: mixing is its own inverse.
+    __device__ static __forceinline__ int along_of(int i) { return B::mixed(i / B::WIDE, i % B::WIDE) % B::WIDE; }
+
+    // The step's pieces to `lds`; `left`: k's from its first to the end (a step beyond the last whole one is cut off).
+    __device__ __forceinline__ void step(i32x4 *lds, int left)
+    {
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(corner), 0, 0x7FFFFFFF, 0x00020000);
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+#pragma unroll
+        for (int u = 0; u < EACH; ++u) {
+            const int i = u * THREADS + threadIdx.x, k = K ? along_of(i) * B::PIECE : i / B::WIDE;
+            const int from = left >= B::STEP || k < left ? at[u] : OUTSIDE;
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void *)(lds + u * THREADS + wave * 64), 16, from, 0, 0, 0);
+        }
+        corner += advance;
+    }
+};
+
+template <typename T, bool AK, bool BK, int TM, int TN, int WM, int WN>
+__global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
+{
+    constexpr int THREADS = 64 * WM * WN, MI = TM / WM / 32, NI = TN / WN / 32;
+    using CA = Copy<T, TM, AK, false, THREADS>;
+    using CB = Copy<T, TN, BK, true, THREADS>;
+    // (arrays of their own, and a loop of two steps: the compiler sees that a step's reads do not wait for the other buffer's copies)
+    __shared__ i32x4 a0[CA::PIECES], a1[CA::PIECES], b0[CB::PIECES], b1[CB::PIECES];
+    const int tiles = a.tiles_m * a.tiles_n, split = blockIdx.x / tiles;
+    int tm, tn;
+    tile_at(tile_of(blockIdx.x % tiles, tiles), a.tiles_m, a.tiles_n, tm, tn);
+    const int row0 = tm * TM, col0 = tn * TN;
+    const int k_begin = split * a.k_split, k_end = a.k - k_begin < a.k_split ? a.k : k_begin + a.k_split;
+    const int wave = threadIdx.x / 64, wm = wave / WN * (TM / WM), wn = wave % WN * (TN / WN);
+    CA ca(static_cast<const T *>(a.a), a.lda, row0, a.m, k_begin);
+    CB cb(static_cast<const T *>(a.b), a.ldb, col0, a.n, k_begin);
+    f32x16 acc[MI][NI] = {};
+    typename CA::F fa[2][MI];
+    typename CB::F fb[2][NI];
+    auto read = [&](const i32x4 *la, const i32x4 *lb, int s, int to) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i) fa[to][i] = CA::read(la, wm + 32 * i, s);
+#pragma unroll
+        for (int j = 0; j < NI; ++j) fb[to][j] = CB::read(lb, wn + 32 * j, s);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto products = [&](int of) {
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = multiply(fb[of][j], fa[of][i], acc[i][j]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // A frag's reads go out before the products of the frag before.  The last frag of a step is in registers before its products start: at that point
+    // the buffer is free for the step after the next, and the next step's first frag can be read.  The copies of one operand go out among those
+    // last products, the other's among the first ones of the next step: all sixteen at once held the products up (8192 x 4096 -> 4096 bf16: dw 231 -> 216 us).
+    int left = k_end - k_begin;
+    auto step = [&](i32x4 *la, i32x4 *lb, i32x4 *next_a, i32x4 *next_b) {
+        read(la, lb, 1, 1);
+        cb.step(next_b, left);
+        products(0);
+        read(la, lb, 2, 0);
+        products(1);
+        read(la, lb, 3, 1);
+        products(0);
+        copies_done();
+        __syncthreads();
+        left -= CA::STEP;
+        read(next_a, next_b, 0, 0);
+        ca.step(la, left);
+        products(1);
+    };
+    // Two steps a turn, the last of them perhaps of zeros: with a step of its own behind the loop the compiler keeps the sums twice (and spills).
+    const int steps = (left + CA::STEP - 1) / CA::STEP;
+    ca.step(a0, left); cb.step(b0, left);
+    copies_done();
+    __syncthreads();
+    left -= CA::STEP;
+    ca.step(a1, left);
+    read(a0, b0, 0, 0);
+    for (int t = 0; t < (steps + 1) / 2; ++t) {
+        step(a0, b0, a1, b1);
+        step(a1, b1, a0, b0);
+    }
+    static_assert(NI == 2 && CA::PIECES >= WM * WN / 2 * FINISH_PIECES, "a wave ends 64 columns, in the tiles' LDS");
+    copies_done();                                  // (zeros for a step that does not come)
+    __syncthreads();
+    f32x4 *room = finish_room<WM * WN>(a0, a1);
+    // (the code once, with the sums moved up: four copies of it are more than the instruction cache holds)
+#pragma unroll 1
+    for (int i = 0; i < MI; ++i) {
+        finish_tile<T>(a, split, row0 + wm + 32 * i, col0 + wn, acc[0][0], acc[0][1], room);
+#pragma unroll
+        for (int u = 0; u + 1 < MI; ++u) { acc[u][0] = acc[u + 1][0]; acc[u][1] = acc[u + 1][1]; }
+    }
 }
 
 // ---- any size, any stride ---------------------------------------------------------------------------------
@@ -267,10 +434,10 @@ __global__ __launch_bounds__(256) void product_any_kernel(ProductArgs a)
                 for (int j = 0; j < 2; ++j) acc[i][j] = multiply(fb[j], fa[i], acc[i][j]);
         }
     }
+    __syncthreads();
+    f32x4 *room = finish_room<4>(la, lb);
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) finish_tile<T>(a, split, row0 + wm + 32 * i, col0 + wn + 32 * j, acc[i][j]);
+    for (int i = 0; i < 2; ++i) finish_tile<T>(a, split, row0 + wm + 32 * i, col0 + wn, acc[i][0], acc[i][1], room);
 }
 
 // Adds the splits' sums in their order and ends them.  A chunk a thread, four for each block of 32 columns (the 8-bit copy needs them side by side).

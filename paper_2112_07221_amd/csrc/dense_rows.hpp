@@ -8,7 +8,7 @@ namespace het {
 
 constexpr int ROW_THREADS = 256;
 constexpr int ROW_WAVES = ROW_THREADS / 64;
-constexpr int ROW_WIDE = 64 * CHUNK * 4;           // widest row that a wave holds: 4 chunks a lane
+constexpr int ROW_WIDE = 64 * CHUNK;               // widest row that a wave holds, a chunk a lane
 constexpr int ROW_WIDEST = 1024 * CHUNK * 4;       // and a workgroup
 constexpr uint32_t PARTIALS = 512;                 // workgroups that leave partial column sums
 
@@ -77,33 +77,34 @@ struct NormArgs {
     float eps;
 };
 
-template <typename TX, typename TY, int NV, bool BLOCK>
-__global__ __launch_bounds__(BLOCK ? 1024 : ROW_THREADS) void norm_kernel(NormArgs a)
+template <typename TX, typename TY, int NV, int MOST, bool WHOLE>
+__global__ __launch_bounds__(MOST) void norm_kernel(NormArgs a)
 {
+    constexpr bool BLOCK = MOST > ROW_THREADS;
     __shared__ float lds[64];
     const int lanes = a.s.lanes, gl = threadIdx.x % lanes, dim = a.s.dim;
     const int64_t row = BLOCK ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (ROW_THREADS / lanes) + threadIdx.x / lanes;
     if (row >= a.rows) return;                     // (whole rows of lanes; a workgroup that holds one row has one)
     const TX *x = static_cast<const TX *>(a.x) + row * a.ldx;
     RowSum<BLOCK> sum(lds, lanes);
+    vec<TX, 8> raw[NV];
     f32x8 v[NV];
     float s = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        const int c = gl + i * lanes, n = chunk_values(c, dim);
-        v[i] = n > 0 ? load_some(x + c * CHUNK, n) : f32x8{};
-    }
+    for (int i = 0; i < NV; ++i) raw[i] = load_raw<WHOLE>(x, gl + i * lanes, dim);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int i = 0; i < NV; ++i) {
+        v[i] = raw_values<WHOLE>(raw[i], gl + i * lanes, dim);
 #pragma unroll
         for (int j = 0; j < 8; ++j) s += v[i][j];
+    }
     const float mean = sum.one(s) / (float)dim;
     s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
         const int n = chunk_values(gl + i * lanes, dim);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { v[i][j] = j < n ? v[i][j] - mean : 0.f; s += v[i][j] * v[i][j]; }
+        for (int j = 0; j < 8; ++j) { v[i][j] = (WHOLE ? n > 0 : j < n) ? v[i][j] - mean : 0.f; s += v[i][j] * v[i][j]; }
     }
     const float rstd = 1.f / sqrtf(sum.one(s) / (float)dim + a.eps);
     if (gl == 0) {
@@ -119,11 +120,11 @@ __global__ __launch_bounds__(BLOCK ? 1024 : ROW_THREADS) void norm_kernel(NormAr
         for (int j = 0; j < 8; ++j) h[j] = v[i][j] * rstd;
         if (a.q && c * CHUNK < a.s.pitch) pack_chunk(a.q + row * a.s.pitch, a.e + row * (a.s.pitch / PACK_BLOCK), c, h);
         if (n <= 0) continue;
-        const f32x8 g = a.gamma ? load_some(a.gamma + c * CHUNK, n) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
-        const f32x8 b = a.beta ? load_some(a.beta + c * CHUNK, n) : f32x8{};
+        const f32x8 g = a.gamma ? load_row<WHOLE>(a.gamma, c, dim) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
+        const f32x8 b = a.beta ? load_row<WHOLE>(a.beta, c, dim) : f32x8{};
 #pragma unroll
         for (int j = 0; j < 8; ++j) h[j] = h[j] * g[j] + b[j];
-        store_some(y + c * CHUNK, h, n);
+        store_row<WHOLE>(y, c, dim, h);
     }
 }
 
@@ -144,10 +145,40 @@ struct NormBackArgs {
     RowShape s;
 };
 
-template <typename TX, typename TY, int NV, bool BLOCK>
-__global__ __launch_bounds__(BLOCK ? 1024 : ROW_THREADS) void norm_back_kernel(NormBackArgs a)
+// What a lane loads of a row: dy, and x or its normalised values in 8 bits.
+template <typename TX, typename TY, int NV, bool KEPT, bool WHOLE>
+struct NormRow {
+    vec<TY, 8> dy[NV];
+    vec<TX, 8> x[KEPT ? 1 : NV];
+    uint64_t q[KEPT ? NV : 1];
+    uint8_t e[KEPT ? NV : 1];
+    float rstd, mean;
+
+    __device__ __forceinline__ void load(const NormBackArgs &a, int64_t row, int gl)
+    {
+        const int lanes = a.s.lanes, dim = a.s.dim;
+        rstd = a.rstd[row];
+        mean = KEPT ? 0.f : a.mean[row];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = gl + i * lanes;
+            dy[i] = load_raw<WHOLE>(static_cast<const TY *>(a.dy) + row * a.lddy, c, dim);
+            if (KEPT) {
+                const int in = c * CHUNK < a.s.pitch ? c : 0;
+                __builtin_memcpy(&q[i], a.q + row * a.s.pitch + in * CHUNK, 8);
+                e[i] = a.e[row * (a.s.pitch / PACK_BLOCK) + (in >> 2)];
+            } else {
+                x[i] = load_raw<WHOLE>(static_cast<const TX *>(a.x) + row * a.ldx, c, dim);
+            }
+        }
+    }
+};
+
+template <typename TX, typename TY, int NV, int MOST, bool KEPT, bool WHOLE>
+__global__ __launch_bounds__(MOST) void norm_back_kernel(NormBackArgs a)
 {
-    extern __shared__ float cols[];                // [2][width], where several rows' lanes share columns
+    constexpr bool BLOCK = MOST > ROW_THREADS;
+    extern __shared__ __attribute__((aligned(16))) float cols[];      // [chunk][dgamma, dbeta][8], where several rows' lanes share columns
     __shared__ float lds[64];
     const int lanes = a.s.lanes, gl = threadIdx.x % lanes, dim = a.s.dim;
     const int64_t per = BLOCK ? 1 : ROW_THREADS / lanes, step = per * gridDim.x;
@@ -155,36 +186,29 @@ __global__ __launch_bounds__(BLOCK ? 1024 : ROW_THREADS) void norm_back_kernel(N
     f32x8 dg[NV], db[NV], gamma[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int c = gl + i * lanes, n = chunk_values(c, dim);
         dg[i] = db[i] = f32x8{};
-        gamma[i] = n <= 0 ? f32x8{} : a.gamma ? load_some(a.gamma + c * CHUNK, n) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
+        gamma[i] = a.gamma ? load_row<WHOLE>(a.gamma, gl + i * lanes, dim) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
     }
-    for (int64_t row = (int64_t)blockIdx.x * per + (BLOCK ? 0 : threadIdx.x / lanes); row < a.rows; row += step) {
-        const TY *dy = static_cast<const TY *>(a.dy) + row * a.lddy;
-        f32x8 d[NV], h[NV];
-        const float rstd = a.rstd[row], mean = a.q ? 0.f : a.mean[row];
+    int64_t row = (int64_t)blockIdx.x * per + (BLOCK ? 0 : threadIdx.x / lanes);
+    NormRow<TX, TY, NV, KEPT, WHOLE> now, next;
+    if (row < a.rows) now.load(a, row, gl);
+    for (; row < a.rows; row += step, now = next) {
+        vec<TX, 8> r[NV];
+        if (a.residual)
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int c = gl + i * lanes, n = chunk_values(c, dim);
-            d[i] = n > 0 ? load_some(dy + c * CHUNK, n) : f32x8{};
-            h[i] = f32x8{};
-            if (n <= 0) continue;
-            if (a.q) {
-                uint64_t q;
-                __builtin_memcpy(&q, a.q + row * a.s.pitch + c * CHUNK, 8);
-                h[i] = unpack_chunk(q, a.e[row * (a.s.pitch / PACK_BLOCK) + (c >> 2)]);
-            } else {
-                h[i] = load_some(static_cast<const TX *>(a.x) + row * a.ldx + c * CHUNK, n);
-            }
-        }
+            for (int i = 0; i < NV; ++i) r[i] = load_raw<WHOLE>(static_cast<const TX *>(a.residual) + row * a.ldr, gl + i * lanes, dim);
+        if (row + step < a.rows) next.load(a, row + step, gl);        // on its way while this row is summed and written
+        f32x8 d[NV], h[NV];
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int n = chunk_values(gl + i * lanes, dim);
+            const int c = gl + i * lanes, n = chunk_values(c, dim);
+            d[i] = raw_values<WHOLE>(now.dy[i], c, dim);
+            h[i] = KEPT ? unpack_chunk(now.q[i], now.e[i]) : raw_values<WHOLE>(now.x[i], c, dim);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (!a.q) h[i][j] = (h[i][j] - mean) * rstd;
-                if (j >= n) { h[i][j] = 0.f; d[i][j] = 0.f; }
+                if (!KEPT) h[i][j] = (h[i][j] - now.mean) * now.rstd;
+                if (WHOLE ? n <= 0 : j >= n) h[i][j] = 0.f;
                 dg[i][j] += d[i][j] * h[i][j];
                 db[i][j] += d[i][j];
                 d[i][j] *= gamma[i][j];
@@ -197,17 +221,16 @@ __global__ __launch_bounds__(BLOCK ? 1024 : ROW_THREADS) void norm_back_kernel(N
         TX *dx = static_cast<TX *>(a.dx) + row * a.lddx;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = gl + i * lanes, n = chunk_values(c, dim);
-            if (n <= 0) continue;
+            const int c = gl + i * lanes;
             f32x8 o;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] = rstd * (d[i][j] - s1 - h[i][j] * s2);
+            for (int j = 0; j < 8; ++j) o[j] = now.rstd * (d[i][j] - s1 - h[i][j] * s2);
             if (a.residual) {
-                const f32x8 r = load_some(static_cast<const TX *>(a.residual) + row * a.ldr + c * CHUNK, n);
+                const f32x8 f = raw_values<WHOLE>(r[i], c, dim);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] += r[j];
+                for (int j = 0; j < 8; ++j) o[j] += f[j];
             }
-            store_some(dx + c * CHUNK, o, n);
+            store_row<WHOLE>(dx, c, dim, o);
         }
     }
     const int width = (dim + CHUNK - 1) / CHUNK * CHUNK;
@@ -222,25 +245,28 @@ __global__ __launch_bounds__(BLOCK ? 1024 : ROW_THREADS) void norm_back_kernel(N
         }
         return;
     }
-    // lanes of a wave that hold the same columns of other rows, then the waves one after the other
+    // lanes of a wave that hold the same columns of other rows, then the waves one after the other (a chunk a lane here)
     for (int o = lanes; o < 64; o <<= 1)
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) { dg[i][j] += __shfl_xor(dg[i][j], o); db[i][j] += __shfl_xor(db[i][j], o); }
+        for (int j = 0; j < 8; ++j) { dg[0][j] += __shfl_xor(dg[0][j], o); db[0][j] += __shfl_xor(db[0][j], o); }
+    const bool mine = (int)threadIdx.x % 64 < lanes && gl * CHUNK < width;
+    f32x4 *at = reinterpret_cast<f32x4 *>(cols) + 4 * gl;
     for (int w = 0; w < ROW_WAVES; ++w) {
-        if ((int)threadIdx.x / 64 == w && (int)threadIdx.x % 64 < lanes)
+        if ((int)threadIdx.x / 64 == w && mine) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int c = gl + i * lanes;
-                if (c * CHUNK >= width) continue;
-                float *p = cols + c * CHUNK, *r = cols + width + c * CHUNK;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) { p[j] = w ? p[j] + dg[i][j] : dg[i][j]; r[j] = w ? r[j] + db[i][j] : db[i][j]; }
+            for (int u = 0; u < 4; ++u) {
+                const f32x8 &s = u < 2 ? dg[0] : db[0];
+                f32x4 v = {s[4 * (u % 2)], s[4 * (u % 2) + 1], s[4 * (u % 2) + 2], s[4 * (u % 2) + 3]};
+                if (w) for (int j = 0; j < 4; ++j) v[j] += at[u][j];
+                at[u] = v;
             }
+        }
         __syncthreads();
     }
-    for (int c = threadIdx.x; c < 2 * width; c += ROW_THREADS) out[c] = cols[c];
+    for (int c = threadIdx.x; c < 2 * width; c += ROW_THREADS) {
+        const int col = c < width ? c : c - width;
+        out[c] = cols[col / CHUNK * 2 * CHUNK + (c < width ? 0 : CHUNK) + col % CHUNK];
+    }
 }
 
 // Column sums of partial[n][sets][width]: set s goes to out[s] (null: nobody asks).  16 columns a workgroup, 16 threads for each of them, which
@@ -292,7 +318,7 @@ struct SlopeArgs {
 
 constexpr int SLOPE_COLS = 32 * CHUNK;
 
-template <typename T, typename TY>
+template <typename T, typename TY, bool WHOLE>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
 {
     __shared__ float lds[8][SLOPE_COLS];
@@ -300,7 +326,7 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     f32x8 s = {};
     if (n > 0)
         for (int64_t row = (int64_t)blockIdx.y * 8 + ry; row < a.rows; row += 8 * (int64_t)gridDim.y) {
-            f32x8 d = load_some(static_cast<const TY *>(a.dy) + row * a.lddy + c * CHUNK, n);
+            f32x8 d = load_row<WHOLE>(static_cast<const TY *>(a.dy) + row * a.lddy, c, a.dim);
             if (a.act != DENSE_ACT_NONE) {
                 f32x8 z;
                 if (a.q) {
@@ -308,14 +334,15 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
                     __builtin_memcpy(&q, a.q + row * a.pitch + c * CHUNK, 8);
                     z = unpack_chunk(q, a.e[row * (a.pitch / PACK_BLOCK) + (c >> 2)]);
                 } else {
-                    z = load_some(static_cast<const T *>(a.z) + row * a.ldz + c * CHUNK, n);
+                    z = load_row<WHOLE>(static_cast<const T *>(a.z) + row * a.ldz, c, a.dim);
                 }
+                z = act_chunk<true>(a.act, z);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) d[j] *= act_slope(a.act, z[j]);
+                for (int j = 0; j < 8; ++j) d[j] *= z[j];
             }
-            if (a.dz) store_some(static_cast<T *>(a.dz) + row * a.lddz + c * CHUNK, d, n);
+            if (a.dz) store_row<WHOLE>(static_cast<T *>(a.dz) + row * a.lddz, c, a.dim, d);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] += j < n ? d[j] : 0.f;
+            for (int j = 0; j < 8; ++j) s[j] += (WHOLE || j < n) ? d[j] : 0.f;
         }
     if (!a.partial) return;
 #pragma unroll
@@ -387,8 +414,9 @@ __global__ __launch_bounds__(256) void expand_kernel(ExpandArgs a)
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += b[j];
     }
+    v = act_chunk<false>(a.act, v);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = within<T>(act_value(a.act, v[j]));
+    for (int j = 0; j < 8; ++j) v[j] = within<T>(v[j]);
     store_some(static_cast<T *>(a.y) + row * a.ldy + c * CHUNK, v, n);
 }
 
