@@ -94,20 +94,44 @@ struct BackPlan {
     ProductPlan dx, dw;
     int slope;                  // workgroups down the rows
     int64_t bias_at, x_at, partial_at, bytes;
+    const void *dz, *x;         // the products' operands
+    int64_t lddz, ldx;
 };
 
-BackPlan back_plan(const het_linear_t *l)
+// sizes_only: the workspace's size is asked for, and nobody knows yet how the operands lie: the larger of what the kernels for either take.
+ProductPlan plan_of(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k, const void *a, int64_t lda, const void *b, int64_t ldb, bool sizes_only)
+{
+    if (!sizes_only)
+        return product_plan(m, n, k, type, a_k, b_k, product_copies(a, lda, (int)(a_k ? k : m), type) && product_copies(b, ldb, (int)(b_k ? k : n), type));
+    ProductPlan p = product_plan(m, n, k, type, a_k, b_k, true);
+    p.partial_bytes = std::max(p.partial_bytes, product_plan(m, n, k, type, a_k, b_k, false).partial_bytes);
+    return p;
+}
+
+BackPlan back_plan(const het_linear_t *l, bool sizes_only)
 {
     BackPlan p;
-    p.dx = product_plan(l->rows, l->in, l->out, l->type, true, false);
-    p.dw = product_plan(l->out, l->in, l->rows, l->type, false, false);
     p.slope = slope_splits(l->rows, l->out);
     p.bias_at = 0;
     p.x_at = l->dbias ? align16((int64_t)p.slope * width_of(l->out) * 4) : 0;
     p.partial_at = p.x_at + (l->xq && l->dw ? align16(l->rows * (int64_t)l->in * size_of(l->type)) : 0);
-    p.bytes = p.partial_at + std::max(l->dx ? p.dx.partial_bytes : 0, l->dw ? p.dw.partial_bytes : 0);
+    p.dz = l->dz ? l->dz : l->dy;
+    p.lddz = l->dz ? l->lddz : l->lddy;
+    p.x = l->xq ? static_cast<const char *>(l->workspace) + p.x_at : static_cast<const char *>(l->x);
+    p.ldx = l->xq ? l->in : l->ldx;
+    p.bytes = p.partial_at;
+    if (l->dx) {
+        p.dx = plan_of(l->rows, l->in, l->out, l->type, true, false, p.dz, p.lddz, l->w, l->ldw, sizes_only);
+        p.bytes = p.partial_at + p.dx.partial_bytes;
+    }
+    if (l->dw) {
+        p.dw = plan_of(l->out, l->in, l->rows, l->type, false, false, p.dz, p.lddz, p.x, p.ldx, sizes_only);
+        p.bytes = std::max(p.bytes, p.partial_at + p.dw.partial_bytes);
+    }
     return p;
 }
+
+ProductPlan forward_plan(const het_linear_t *l, bool sizes_only) { return plan_of(l->rows, l->out, l->in, l->type, true, true, l->x, l->ldx, l->w, l->ldw, sizes_only); }
 
 bool workspace_ok(const void *ws, int64_t have, int64_t need) { return need == 0 || (ws && aligned16(ws) && have >= need); }
 
@@ -185,8 +209,7 @@ int het_expand(const int8_t *q, const uint8_t *e, int64_t rows, int32_t dim, con
 int64_t het_linear_workspace(const het_linear_t *l, int32_t backward)
 {
     if (!linear_sizes(l)) return HET_EINVAL;
-    if (backward) return back_plan(l).bytes;
-    return product_plan(l->rows, l->out, l->in, l->type, true, true).partial_bytes;
+    return backward ? back_plan(l, true).bytes : forward_plan(l, true).partial_bytes;
 }
 
 int het_linear(const het_linear_t *l, void *hip_stream)
@@ -195,7 +218,7 @@ int het_linear(const het_linear_t *l, void *hip_stream)
     if (l->ldx < l->in || l->ldw < l->in || l->ldy < l->out || (l->residual && l->ld_residual < l->out) || (l->z && l->ldz < l->out) || !l->zq != !l->ze) return HET_EINVAL;
     if (l->rows == 0) return HET_OK;
     if (!l->x || !l->w || !l->y || !aligned16(l->zq)) return HET_EINVAL;
-    const ProductPlan p = product_plan(l->rows, l->out, l->in, l->type, true, true);
+    const ProductPlan p = forward_plan(l, false);
     if (!p.ok || !workspace_ok(l->workspace, l->workspace_bytes, p.partial_bytes)) return HET_EINVAL;
     ProductArgs a{};
     a.a = l->x; a.lda = l->ldx; a.b = l->w; a.ldb = l->ldw;
@@ -225,7 +248,7 @@ int het_linear_backward(const het_linear_t *l, void *hip_stream)
         if (!l->dy || (has_act && !l->zq && !l->z) || (has_act && !aligned16(l->zq))) return HET_EINVAL;
         if ((l->dx && !l->w) || (l->dw && !l->xq && !l->x) || (l->dw && !aligned16(l->xq))) return HET_EINVAL;
     }
-    const BackPlan p = back_plan(l);
+    const BackPlan p = back_plan(l, false);
     if ((l->dx && !p.dx.ok) || (l->dw && !p.dw.ok) || !workspace_ok(l->workspace, l->workspace_bytes, p.bytes)) return HET_EINVAL;
     if (!some && !l->dw && !l->dbias) return HET_OK;
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
@@ -241,11 +264,9 @@ int het_linear_backward(const het_linear_t *l, void *hip_stream)
         with_types(l->y_type, l->type, [&](auto ty, auto t) { launch_slope<typename decltype(t)::type, typename decltype(ty)::type>(s, grid, st); });
         if (l->dbias) launch_column_sum(s.partial, p.slope, 1, l->out, l->dbias, nullptr, st);
     }
-    const void *dz = dz_is_dy ? l->dy : l->dz;
-    const int64_t lddz = dz_is_dy ? l->lddy : l->lddz;
     if (l->dx && some) {
         ProductArgs a{};
-        a.a = dz; a.lda = lddz; a.b = l->w; a.ldb = l->ldw;
+        a.a = p.dz; a.lda = p.lddz; a.b = l->w; a.ldb = l->ldw;
         a.partial = reinterpret_cast<float *>(ws + p.partial_at);
         a.f.y = l->dx; a.f.ldy = l->lddx; a.f.y_f32 = l->type == HET_F32;
         launch_product(a, p.dx, l->type, true, false, st);
@@ -256,8 +277,7 @@ int het_linear_backward(const het_linear_t *l, void *hip_stream)
             if (rc != HET_OK) return rc;
         }
         ProductArgs a{};
-        a.a = dz; a.lda = lddz;
-        a.b = l->xq ? static_cast<const void *>(ws + p.x_at) : l->x; a.ldb = l->xq ? l->in : l->ldx;
+        a.a = p.dz; a.lda = p.lddz; a.b = p.x; a.ldb = p.ldx;
         a.partial = reinterpret_cast<float *>(ws + p.partial_at);
         a.f.y = l->dw; a.f.ldy = l->lddw; a.f.y_f32 = l->type == HET_F32;
         launch_product(a, p.dw, l->type, false, false, st);

@@ -7,14 +7,17 @@ namespace het {
 
 struct ProductPlan {
     bool ok;                    // the grid fits
-    int few;                    // 16-row tiles of the kernel for few rows; 0: another kernel
-    int tile;                   // edge of product_kernel's tile
+    int small_m, small_n;       // 16-row and -column tiles of product_small_kernel's workgroups; 0: another kernel
+    bool aligned;               // product_kernel, else product_any_kernel
+    int tile;                   // its tile's edge
     int m, n, k, splits, k_split;
     int64_t partial_bytes;
 };
 
 // D[m][n] over k; `a_k`, `b_k`: the operands are read along k.  type: HET_F32, ...
-ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k);
+// aligned: both operands are as product_copies asks.
+ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k, bool aligned);
+bool product_copies(const void *p, int64_t ld, int width, int type);
 
 // Fills in the sizes of `a` and enqueues the product.
 void launch_product(ProductArgs a, const ProductPlan &p, int type, bool a_k, bool b_k, hipStream_t st);

@@ -10,7 +10,7 @@ static_assert(HET_PARTS == HET_PRODUCT_PARTS, "the build compiles other parts th
 
 namespace het {
 
-template <typename T> void launch_product_of(const ProductArgs &a, const ProductPlan &p, bool direct, bool a_k, bool b_k, hipStream_t st);
+template <typename T> void launch_product_of(const ProductArgs &a, const ProductPlan &p, bool a_k, bool b_k, hipStream_t st);
 
 #if HET_PART == 0
 using PartType = float;
@@ -20,29 +20,32 @@ using PartType = bf16;
 using PartType = f16;
 #endif
 
-template <typename T, int NT>
-static void launch_few(const ProductArgs &a, int mt, hipStream_t st)
+template <typename T, int MT, int NT>
+static void launch_small(const ProductArgs &a, bool a_k, bool b_k, hipStream_t st)
 {
-    const uint32_t grid = (uint32_t)((a.n + 16 * NT - 1) / (16 * NT));
-    if (mt == 1) product_few_kernel<T, 1, NT><<<grid, 64 * FEW_WAVES, 0, st>>>(a);
-    else if (mt == 2) product_few_kernel<T, 2, NT><<<grid, 64 * FEW_WAVES, 0, st>>>(a);
-    else product_few_kernel<T, 4, NT><<<grid, 64 * FEW_WAVES, 0, st>>>(a);
+    const uint32_t grid = (uint32_t)(a.tiles_m * a.tiles_n);
+    if (a_k && b_k) product_small_kernel<T, true, true, MT, NT><<<grid, 64 * SMALL_WAVES, 0, st>>>(a);
+    else if constexpr (MT == 2) {
+        if (a_k) product_small_kernel<T, true, false, MT, NT><<<grid, 64 * SMALL_WAVES, 0, st>>>(a);
+        else product_small_kernel<T, false, false, MT, NT><<<grid, 64 * SMALL_WAVES, 0, st>>>(a);
+    }
 }
 
 template <typename T>
-void launch_product_of(const ProductArgs &a, const ProductPlan &p, bool direct, bool a_k, bool b_k, hipStream_t st)
+void launch_product_of(const ProductArgs &a, const ProductPlan &p, bool a_k, bool b_k, hipStream_t st)
 {
-    if (p.few) {
-        if (a.f.q) launch_few<T, 2>(a, p.few, st);
-        else launch_few<T, 1>(a, p.few, st);
+    if (p.small_m) {
+        const bool wide = p.small_n == 2 || a.f.q;          // (a block of the 8-bit form needs its 32 columns together)
+        if (p.small_m == 1) { if (wide) launch_small<T, 1, 2>(a, a_k, b_k, st); else launch_small<T, 1, 1>(a, a_k, b_k, st); }
+        else { if (wide) launch_small<T, 2, 2>(a, a_k, b_k, st); else launch_small<T, 2, 1>(a, a_k, b_k, st); }
         return;
     }
     const uint32_t grid = (uint32_t)(a.tiles_m * a.tiles_n * a.splits);
-    if (direct && p.tile == 256) {
+    if (p.aligned && p.tile == 256) {
         if (a_k && b_k) product_kernel<T, true, true, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
         else if (a_k) product_kernel<T, true, false, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
         else product_kernel<T, false, false, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
-    } else if (direct) {
+    } else if (p.aligned) {
         if (a_k && b_k) product_kernel<T, true, true, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
         else if (a_k) product_kernel<T, true, false, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
         else product_kernel<T, false, false, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
@@ -55,46 +58,57 @@ void launch_product_of(const ProductArgs &a, const ProductPlan &p, bool direct, 
     }
 }
 
-template void launch_product_of<PartType>(const ProductArgs &, const ProductPlan &, bool, bool, bool, hipStream_t);
+template void launch_product_of<PartType>(const ProductArgs &, const ProductPlan &, bool, bool, hipStream_t);
 
 #if HET_PART == 0
-extern template void launch_product_of<bf16>(const ProductArgs &, const ProductPlan &, bool, bool, bool, hipStream_t);
-extern template void launch_product_of<f16>(const ProductArgs &, const ProductPlan &, bool, bool, bool, hipStream_t);
+extern template void launch_product_of<bf16>(const ProductArgs &, const ProductPlan &, bool, bool, hipStream_t);
+extern template void launch_product_of<f16>(const ProductArgs &, const ProductPlan &, bool, bool, hipStream_t);
 
-constexpr int FEW_ROWS = 64;
 constexpr int64_t CUS = 256;
 
-// Microseconds a product takes with tiles of 256 or 128 and its k's split, by the times measured at 2048 .. 8192 rows and columns, 64 .. 8192
-// k's, bf16 (fp32's steps take 4.8 times as long): a tile of 256 has a compute unit to itself, of 128 two share one.  Adding up the splits costs a
-// launch and the sums' way through memory.
-static double product_us(int tile, int64_t tiles, int64_t splits, int64_t steps, int64_t m, int64_t n, bool f32)
+// Microseconds a product takes with tiles of 256 or 128 and its k's split, by the times measured at 64 .. 8192 rows, columns and k's in bf16 and
+// fp32: a tile of 256 has a compute unit to itself, of 128 two share one.  Adding up the splits costs a launch and the sums' way through memory.
+static double tiles_us(int tile, int64_t tiles, int64_t splits, int64_t steps, int64_t m, int64_t n, bool f32, bool aligned)
 {
-    const double s = (double)((steps + splits - 1) / splits) * (f32 ? 4.8 : 1.0);
-    const int64_t groups = tiles * splits, turns = groups / CUS, more = groups % CUS != 0;
+    const double s = (double)((steps + splits - 1) / splits) * (aligned ? 1.0 : f32 ? 1.2 : 2.0);
+    const int64_t groups = tiles * splits, turns = (groups + CUS - 1) / CUS;
     double us = 0;
-    if (tile == 256) us = (double)(turns + more) * (10 + 1.5 * s);
-    else us = (double)((turns + more) / 2) * (6 + 0.86 * s) + (double)((turns + more) % 2) * (4 + 0.5 * s);
+    if (tile == 256) us = (double)turns * (10 + (f32 ? 7.3 : 1.5) * s);
+    else us = (double)(turns / 2) * (6 + (f32 ? 4.1 : 0.86) * s) + (double)(turns % 2) * (4 + (f32 ? 2.1 : 0.5) * s);
     return splits > 1 ? us + 4 + (double)splits * (double)m * (double)n * 2e-6 : us;
 }
 
-ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k)
+// ... and with product_small_kernel: its waves' turns through k (a step is a span, two of them at a time), a thousand workgroups at a time, and the
+// operands out of the L2 once for every 32 rows or columns.  1001 x 500 -> 250 in fp16: 7.6 .. 8.4 us a product, tiles 16.6 .. 20.4; 2048 x 1024 ->
+// 1024 in bf16: 30.6, tiles 11.4; a single token 1664 -> 1024: 7.9, tiles 12.7 (each with the launch).
+static double small_us(int64_t steps, int64_t m, int64_t n, int64_t k, bool a_k, bool b_k, bool f32)
+{
+    const int64_t high = a_k && b_k && m <= 16 ? 16 : (m + 31) / 32 * 32, wide = (n + 31) / 32 * 32;
+    const double turn = a_k && b_k ? 1.0 : a_k ? 1.5 : 2.0, each = f32 ? 28e-9 : a_k && b_k ? 12e-9 : 20e-9;
+    return 1 + turn * (double)((steps + 2 * SMALL_WAVES - 1) / (2 * SMALL_WAVES)) + 4.0 / 1024 * (double)high * (double)wide / 1024 +
+           each * (double)high * (double)wide * (double)k;
+}
+
+ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k, bool aligned)
 {
     ProductPlan p{};
+    p.aligned = aligned;
     p.m = (int)m; p.n = (int)n; p.k = (int)k;
     p.splits = 1; p.k_split = (int)k; p.tile = ANY_TILE;
     p.ok = true;
-    if (a_k && b_k && m <= FEW_ROWS) {
-        p.few = m <= 16 ? 1 : m <= 32 ? 2 : 4;
-        return p;
-    }
     const int64_t step = type == HET_F32 ? 32 : 64, steps = (k + step - 1) / step;
     double best = 1e30;
-    for (int tile = 256; tile >= 128; tile /= 2) {
+    for (int tile = aligned ? 256 : ANY_TILE; tile >= 128; tile /= 2) {
         const int64_t tiles = ((m + tile - 1) / tile) * ((n + tile - 1) / tile);
         for (int64_t splits = 1; splits <= 32 && (splits == 1 || (splits * 4 <= steps && tiles * splits <= 2 * CUS)); ++splits) {
-            const double us = product_us(tile, tiles, splits, steps, m, n, type == HET_F32);
+            const double us = tiles_us(tile, tiles, splits, steps, m, n, type == HET_F32, aligned);
             if (us < best) { best = us; p.tile = tile; p.splits = (int)splits; }
         }
+    }
+    if (small_us(steps, m, n, k, a_k, b_k, type == HET_F32) < best) {
+        p.small_m = a_k && b_k && m <= 16 ? 1 : 2;
+        p.small_n = ((m + 31) / 32) * ((n + 31) / 32) < CUS ? 1 : 2;
+        p.splits = 1;
     }
     p.k_split = (int)((steps + p.splits - 1) / p.splits * step);
     p.splits = (int)std::max<int64_t>(1, (k + p.k_split - 1) / std::max(p.k_split, 1));
@@ -104,22 +118,21 @@ ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bo
 }
 
 // Whether product_kernel takes an operand as it lies: rows at multiples of 16 bytes, whole pieces of them along k or across, and a tile within 2 GB.
-static bool copies(const void *p, int64_t ld, int width, int rows_of_tile, int64_t size)
+bool product_copies(const void *p, int64_t ld, int width, int type)
 {
-    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * size % 16 == 0 && width * size % 16 == 0 && rows_of_tile * ld * size < (1ll << 31);
+    const int64_t size = type == HET_F32 ? 4 : 2;
+    return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * size % 16 == 0 && width * size % 16 == 0 && 256 * ld * size < (1ll << 31);
 }
 
 void launch_product(ProductArgs a, const ProductPlan &p, int type, bool a_k, bool b_k, hipStream_t st)
 {
     a.m = p.m; a.n = p.n; a.k = p.k;
     a.splits = p.splits; a.k_split = p.k_split;
-    const int64_t size = type == HET_F32 ? 4 : 2;
-    const bool direct = copies(a.a, a.lda, a_k ? a.k : a.m, 256, size) && copies(a.b, a.ldb, b_k ? a.k : a.n, 256, size);
-    const int tile = direct ? p.tile : ANY_TILE;
-    a.tiles_m = (a.m + tile - 1) / tile; a.tiles_n = (a.n + tile - 1) / tile;
-    if (type == HET_F32) launch_product_of<float>(a, p, direct, a_k, b_k, st);
-    else if (type == HET_BF16) launch_product_of<bf16>(a, p, direct, a_k, b_k, st);
-    else launch_product_of<f16>(a, p, direct, a_k, b_k, st);
+    const int tile = p.tile, high = p.small_m ? 16 * p.small_m : tile, wide = p.small_m ? 16 * (a.f.q ? 2 : p.small_n) : tile;
+    a.tiles_m = (a.m + high - 1) / high; a.tiles_n = (a.n + wide - 1) / wide;
+    if (type == HET_F32) launch_product_of<float>(a, p, a_k, b_k, st);
+    else if (type == HET_BF16) launch_product_of<bf16>(a, p, a_k, b_k, st);
+    else launch_product_of<f16>(a, p, a_k, b_k, st);
 }
 #endif
 

@@ -114,22 +114,25 @@ struct Tile {
         if (sizeof(T) == 2) return r * WIDE + (c ^ (4 * (r & 3)));
         return r * WIDE + (c ^ (8 * ((r >> 2) & 1)));
     }
-    // Piece `i` of the tile (0 .. PIECES - 1) from memory: rows [row0, rows), k's [k0, k_end); what lies outside is zero.
+    // Piece `i` of the tile (0 .. PIECES - 1) from memory: rows [row0, rows), k's [k0, k_end).  k's outside are zero; rows outside are the last row's
+    // copies (what comes of them is not stored).  A piece that would cross the end of a row in memory is the row's last 16 bytes, shifted: no lane takes a
+    // branch of its own, and the loads of all pieces are under way together.
     __device__ static __forceinline__ i32x4 load(const T *p, int64_t ld, int i, int row0, int rows, int k0, int k_end)
     {
         const int along = i % WIDE, down = i / WIDE;
-        const int outer = (K ? row0 : k0) + down, inner = (K ? k0 : row0) + along * PIECE;
-        const int left = (K ? k_end : rows) - inner;
-        vec<T, PIECE> v = {};
-        if (outer < (K ? rows : k_end) && left > 0) {
-            const T *at = p + (int64_t)outer * ld + inner;
-            if (left >= PIECE) {
-                __builtin_memcpy(&v, at, 16);
-            } else {
+        const int outer = (K ? row0 : k0) + down, inner = (K ? k0 : row0) + along * PIECE, most = K ? rows : k_end, end = K ? k_end : rows;
+        const T *row = p + (int64_t)(outer < most ? outer : most - 1) * ld;
+        if (end < PIECE) {                                        // the whole row is less than a piece
+            vec<T, PIECE> v = {};
 #pragma unroll
-                for (int j = 0; j < PIECE - 1; ++j) if (j < left) v[j] = at[j];
-            }
+            for (int j = 0; j < PIECE - 1; ++j) if (inner + j < end && outer < most) v[j] = row[inner + j];
+            return __builtin_bit_cast(i32x4, v);
         }
+        const int from = inner < end - PIECE ? inner : end - PIECE, over = inner - from;
+        unsigned __int128 v;
+        __builtin_memcpy(&v, row + from, 16);
+        if (end % PIECE) v >>= over < PIECE ? 8 * (int)sizeof(T) * over : 0;
+        if (over >= PIECE || (!K && outer >= most)) v = 0;
         return __builtin_bit_cast(i32x4, v);
     }
     __device__ static __forceinline__ int place(int i) { return mixed(i / WIDE, i % WIDE); }
@@ -462,69 +465,111 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a)
     finish_value<T>(a.f, row, col, n, v);
 }
 
-// ---- few rows ---------------------------------------------------------------------------------------------
-// Up to 16 MT rows (a request's candidates, a single token): bound by reading w once.  A workgroup takes 16 NT rows of w, its waves share
-// k; operands go from memory into the matrix instructions' registers, and the waves' sums meet in LDS.
-constexpr int FEW_WAVES = 8;
+// ---- few rows, or small products --------------------------------------------------------------------------
+// Bound by latency, or by reading w once for a request's few rows.  A workgroup takes 16 MT x 16 NT of D and its waves share k, each every
+// SMALL_WAVES-th span of 128 bytes; operands go from memory into the matrix instructions' registers, two spans at a time, and the waves' sums meet in
+// LDS.  A lane's two pieces of a span lie side by side, so that the four lanes of a row take whole lines.
+constexpr int SMALL_WAVES = 8;
 
-template <typename T, int MT, int NT>
-__global__ __launch_bounds__(64 * FEW_WAVES) void product_few_kernel(ProductArgs a)
-{
-    constexpr int PIECE = 16 / (int)sizeof(T), SPAN = 4 * PIECE;        // k's of a lane's piece, and of an instruction's four pieces
+template <typename T, bool K>
+struct Direct {
+    static constexpr int PIECE = 16 / (int)sizeof(T);
     using F = typename Frag<T>::type;
-    __shared__ float lds[FEW_WAVES][16 * MT][16 * NT + 4];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, r = lane % 16, g = lane / 16, col0 = blockIdx.x * 16 * NT;
-    const T *pa[MT], *pb[NT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) pa[i] = static_cast<const T *>(a.a) + (int64_t)(16 * i + r < a.m ? 16 * i + r : 0) * a.lda;
-#pragma unroll
-    for (int i = 0; i < NT; ++i) pb[i] = static_cast<const T *>(a.b) + (int64_t)(col0 + 16 * i + r < a.n ? col0 + 16 * i + r : 0) * a.ldb;
-    f32x4 acc[MT][NT] = {};
-    const int whole = a.k / SPAN;                     // instructions' spans without an edge
-#pragma unroll 4
-    for (int t = wave; t < whole; t += FEW_WAVES) {
-        const int k = t * SPAN + g * PIECE;
-        F fa[MT], fb[NT];
-#pragma unroll
-        for (int i = 0; i < NT; ++i) __builtin_memcpy(&fb[i], pb[i] + k, 16);
-#pragma unroll
-        for (int i = 0; i < MT; ++i) __builtin_memcpy(&fa[i], pa[i] + k, 16);
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) acc[i][j] = multiply_small(fb[j], fa[i], acc[i][j]);
+    const T *p;                  // the lane's row, or its column of the first row of k's
+    int64_t ld;
+    __device__ __forceinline__ void set(const T *base, int64_t ld_, int row, int rows)
+    {
+        ld = ld_;
+        const int r = row < rows ? row : rows - 1;          // (rows behind the last one are its copies; what comes of them is not stored)
+        p = base + (K ? (int64_t)r * ld : (int64_t)r);
     }
-    if (whole * SPAN < a.k && wave == whole % FEW_WAVES) {
-        const int k = whole * SPAN + g * PIECE, left = a.k - k;
-        F fa[MT], fb[NT];
+    __device__ __forceinline__ F load(int k) const
+    {
+        F f;
+        if (K) __builtin_memcpy(&f, p + k, 16);
+        else
 #pragma unroll
-        for (int i = 0; i < NT; ++i)
+            for (int j = 0; j < PIECE; ++j) f[j] = p[(k + j) * ld];
+        return f;
+    }
+    __device__ __forceinline__ F load_edge(int k, int end) const      // zero from `end` on
+    {
+        F f;
 #pragma unroll
-            for (int j = 0; j < PIECE; ++j) fb[i][j] = j < left ? pb[i][k + j] : (T)0.f;
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < PIECE; ++j) fa[i][j] = j < left ? pa[i][k + j] : (T)0.f;
+        for (int j = 0; j < PIECE; ++j) f[j] = k + j < end ? p[K ? (int64_t)(k + j) : (k + j) * ld] : (T)0.f;
+        return f;
+    }
+};
+
+template <typename T, bool AK, bool BK, int MT, int NT>
+__global__ __launch_bounds__(64 * SMALL_WAVES) void product_small_kernel(ProductArgs a)
+{
+    using DA = Direct<T, AK>;
+    using DB = Direct<T, BK>;
+    constexpr int SPAN = 8 * DA::PIECE, AHEAD = MT * NT == 1 ? 4 : 2;
+    __shared__ float lds[SMALL_WAVES][16 * MT][16 * NT + 4];
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
+    const int row0 = blockIdx.x / a.tiles_n * 16 * MT, col0 = blockIdx.x % a.tiles_n * 16 * NT;
+    f32x4 acc[MT][NT] = {};
+    auto products = [&](const typename DA::F *fa, const typename DB::F *fb) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
             for (int j = 0; j < NT; ++j) acc[i][j] = multiply_small(fb[j], fa[i], acc[i][j]);
+    };
+    DA da[MT];
+    DB db[NT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) da[i].set(static_cast<const T *>(a.a), a.lda, row0 + 16 * i + r, a.m);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) db[j].set(static_cast<const T *>(a.b), a.ldb, col0 + 16 * j + r, a.n);
+    const int whole = a.k / SPAN;                     // spans without an edge
+    for (int t = wave; t < whole; t += AHEAD * SMALL_WAVES) {
+        typename DA::F fa[AHEAD][2][MT];
+        typename DB::F fb[AHEAD][2][NT];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int at = t + u * SMALL_WAVES, k = (at < whole ? at : t) * SPAN + 2 * g * DA::PIECE;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) fb[u][s][j] = db[j].load(k + s * DA::PIECE);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) fa[u][s][i] = da[i].load(k + s * DA::PIECE);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u)
+            if (t + u * SMALL_WAVES < whole) { products(fa[u][0], fb[u][0]); products(fa[u][1], fb[u][1]); }
+    }
+    if (whole * SPAN < a.k && wave == whole % SMALL_WAVES) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int k = whole * SPAN + (2 * g + s) * DA::PIECE;
+            typename DA::F fa[MT];
+            typename DB::F fb[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) fb[j] = db[j].load_edge(k, a.k);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) fa[i] = da[i].load_edge(k, a.k);
+            products(fa, fb);
+        }
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
         for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4 *>(&lds[wave][16 * i + r][16 * j + 4 * g]) = acc[i][j];
     __syncthreads();
-    const int c = threadIdx.x % (2 * NT), row = threadIdx.x / (2 * NT);
-    if (row >= 16 * MT || row >= a.m) return;
+    const int c = threadIdx.x % (2 * NT), at = threadIdx.x / (2 * NT), row = row0 + at;
+    if (at >= 16 * MT || row >= a.m) return;
     const int col = col0 + c * CHUNK, n = a.n - col;
     f32x8 v = {};
 #pragma unroll
-    for (int w = 0; w < FEW_WAVES; ++w)
+    for (int w = 0; w < SMALL_WAVES; ++w)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += lds[w][row][c * CHUNK + j];
+        for (int j = 0; j < 8; ++j) v[j] += lds[w][at][c * CHUNK + j];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < n ? v[j] : 0.f;      // (rows of w behind the last one were read as its first)
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? v[j] : 0.f;
     v = finish_bias(a.f, col, n, v);
     if (NT == 2 && a.f.q) pack_chunk(a.f.q + (int64_t)row * a.f.pitch, a.f.e + (int64_t)row * (a.f.pitch / PACK_BLOCK), col / CHUNK, v);
     finish_value<T>(a.f, row, col, n, v);

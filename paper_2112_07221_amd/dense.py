@@ -10,6 +10,8 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import functools
+import struct
 
 from . import hetcache
 from .hetcache import HET_OK, HetError
@@ -22,22 +24,24 @@ EXPORTS = ("het_layer_norm", "het_layer_norm_backward", "het_layer_norm_workspac
            "het_linear_backward", "het_linear_workspace")
 
 
-class Linear(C.Structure):
-    """het_linear_t."""
-    _fields_ = [("rows", C.c_int64), ("inp", C.c_int32), ("out", C.c_int32), ("type", C.c_int32), ("y_type", C.c_int32),
-                ("act", C.c_int32), ("x_act", C.c_int32)] + \
-               [(n, C.c_int64 if n.startswith("ld") else C.c_void_p) for n in (
-                   "x", "ldx", "xq", "xe", "x_gamma", "x_beta", "w", "ldw", "bias", "residual", "ld_residual", "y", "ldy", "z", "ldz",
-                   "zq", "ze", "dy", "lddy", "dz", "lddz", "dx", "lddx", "dw", "lddw", "dbias", "workspace")] + \
-               [("workspace_bytes", C.c_int64)]
+# het_linear_t: the header's fields in order; `ld*` and sizes are whole numbers, the others pointers
+LINEAR_FIELDS = ("rows", "inp", "out", "type", "y_type", "act", "x_act", "x", "ldx", "xq", "xe", "x_gamma", "x_beta", "w", "ldw", "bias", "residual",
+                 "ld_residual", "y", "ldy", "z", "ldz", "zq", "ze", "dy", "lddy", "dz", "lddz", "dx", "lddx", "dw", "lddw", "dbias", "workspace",
+                 "workspace_bytes")
+_linear_t = struct.Struct("@q6i28q")
 
 
-_lib = _torch = _types = _current_device = _raw_stream = None
+def linear_struct(**fields):
+    """het_linear_t with these fields (None: NULL), the others 0."""
+    return _linear_t.pack(*(fields.get(n) or 0 for n in LINEAR_FIELDS))
+
+
+_lib = _torch = _types = _tensor = _f32 = _current_device = _raw_stream = None
 
 
 def load() -> C.CDLL:
     """The library, with the dense layers' entry points declared."""
-    global _lib, _torch, _types, _current_device, _raw_stream
+    global _lib, _torch, _types, _tensor, _f32, _current_device, _raw_stream
     if _lib is not None:
         return _lib
     lib = hetcache.load()
@@ -48,12 +52,13 @@ def load() -> C.CDLL:
     lib.het_layer_norm_workspace.argtypes = [i64, i32]
     lib.het_pack.argtypes = [p, i32, i64, p, p, i64, i32, p]
     lib.het_expand.argtypes = [p, p, i64, i32, p, p, i32, p, i32, i64, p]
-    lib.het_linear.argtypes = [C.POINTER(Linear), p]
-    lib.het_linear_backward.argtypes = [C.POINTER(Linear), p]
-    lib.het_linear_workspace.argtypes = [C.POINTER(Linear), i32]
+    lib.het_linear.argtypes = [p, p]
+    lib.het_linear_backward.argtypes = [p, p]
+    lib.het_linear_workspace.argtypes = [p, i32]
     for name in EXPORTS:
         getattr(lib, name).restype = i64 if name.endswith("_workspace") else C.c_int
     _torch, _types = torch, {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
+    _tensor, _f32 = torch.Tensor, torch.float32
     _current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
     _lib = lib
     return lib
@@ -79,63 +84,80 @@ class Packed:
 
 
 # ---- checks: what the library cannot see from pointers ------------------------------------------------
-def _device(t, what):
-    if not isinstance(t, _torch.Tensor) or not t.is_cuda:
+# A small call is launches and these lines, so they ask torch for each property once.
+def _not_here(t, what):
+    if not isinstance(t, _tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a tensor on the GPU")
-    if t.get_device() != _current_device():
-        raise ValueError(f"{what} is on another device than the current one")
-    return t
+    raise ValueError(f"{what} is on another device than the current one")
 
 
-def _matrix(t, what, rows, dim, dtype=None):
+def _here(t, what):
+    """The current device, which `t` has to be on."""
+    if isinstance(t, Packed):
+        t = t.q
+    if not isinstance(t, _tensor) or not t.is_cuda:
+        raise TypeError(f"{what} must be on the GPU")
+    dev = _current_device()
+    if t.get_device() != dev:
+        _not_here(t, what)
+    return dev
+
+
+def _matrix(t, what, rows, dim, dev, dtype=None):
     """(pointer, row distance, type) of a [rows, dim] matrix."""
-    _device(t, what)
-    kind = _types.get(t.dtype)
-    if kind is None or (dtype is not None and t.dtype != dtype):
+    if not isinstance(t, _tensor) or t.get_device() != dev:
+        _not_here(t, what)
+    have = t.dtype
+    kind = _types.get(have)
+    if kind is None or (dtype is not None and have is not dtype):
         raise TypeError(f"{what} must be {dtype or 'float32, bfloat16 or float16'}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != dim:
+    if t.shape != (rows, dim):
         raise ValueError(f"{what} must be a matrix of {rows} rows of {dim} values")
     ld, along = t.stride()
     if along != 1 and dim > 1:
         raise ValueError(f"the values of a row of {what} must lie side by side")
-    return t.data_ptr(), (ld if rows > 1 else max(ld, dim)), kind
+    return t.data_ptr(), ld if rows > 1 or ld > dim else dim, kind
 
 
-def _vector(t, what, n):
+def _vector(t, what, n, dev):
     """Pointer of a contiguous fp32 vector of n values; None stays None."""
     if t is None:
         return None
-    _device(t, what)
-    if t.dtype != _torch.float32 or t.numel() != n or not t.is_contiguous():
+    if not isinstance(t, _tensor) or t.get_device() != dev:
+        _not_here(t, what)
+    if t.dtype is not _f32 or t.numel() != n or not t.is_contiguous():
         raise TypeError(f"{what} must be a contiguous float32 vector of {n} values")
     return t.data_ptr()
 
 
-def _packed(p, what, rows, dim):
+def _packed(p, what, rows, dim, dev):
     """(q, e) pointers; None gives None twice."""
     if p is None:
         return None, None
     pitch = -(-dim // PACK_BLOCK) * PACK_BLOCK
-    for t, dtype, width in ((_device(p.q, what), _torch.int8, pitch), (_device(p.e, what), _torch.uint8, pitch // PACK_BLOCK)):
-        if p.dim != dim or t.dtype != dtype or t.shape != (rows, width) or not t.is_contiguous():
-            raise ValueError(f"{what} must be the 8-bit form of a matrix of {rows} rows of {dim} values")
-    return p.q.data_ptr(), p.e.data_ptr()
+    q, e = p.q, p.e
+    for t in (q, e):
+        if not isinstance(t, _tensor) or t.get_device() != dev:
+            _not_here(t, what)
+    if p.dim != dim or q.dtype is not _torch.int8 or e.dtype is not _torch.uint8 or q.shape != (rows, pitch) or e.shape != (rows, pitch // PACK_BLOCK) or \
+            not q.is_contiguous() or not e.is_contiguous():
+        raise ValueError(f"{what} must be the 8-bit form of a matrix of {rows} rows of {dim} values")
+    return q.data_ptr(), e.data_ptr()
 
 
-def _stream(stream):
-    return _raw_stream(_current_device()) if stream is None else stream.cuda_stream
+def _stream(stream, dev):
+    return _raw_stream(dev) if stream is None else stream.cuda_stream
 
 
-def _scratch(need, workspace, stream):
+def _scratch(need, workspace, stream, dev):
     """(tensor, pointer, bytes) of a call's workspace."""
-    if need < 0:
-        raise HetError(need, "workspace")
     if workspace is not None:
-        _device(workspace, "workspace")
+        if not isinstance(workspace, _tensor) or workspace.get_device() != dev:
+            _not_here(workspace, "workspace")
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
         return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    if need == 0:
+    if need <= 0:                                          # (below 0: sizes that the call itself refuses)
         return None, None, 0
     with contextlib.nullcontext() if stream is None else _torch.cuda.stream(stream):
         t = _torch.empty(need, dtype=_torch.uint8, device="cuda")
@@ -150,7 +172,7 @@ def _rc(status, what):
 def _shape(t, what):
     if isinstance(t, Packed):
         return t.rows, t.dim
-    if not isinstance(t, _torch.Tensor) or t.dim() != 2:
+    if not isinstance(t, _tensor) or t.dim() != 2:
         raise TypeError(f"{what} must be a matrix on the GPU")
     return t.shape
 
@@ -160,13 +182,16 @@ def layer_norm(x, gamma, beta, y, mean=None, rstd=None, packed=None, eps=1e-5, s
     """y = gamma (x - mean) rstd + beta by rows (het_layer_norm).  packed (a Packed or None) keeps the normalised rows in 8 bits."""
     lib = _lib or load()
     rows, dim = _shape(x, "x")
-    px, ldx, tx = _matrix(x, "x", rows, dim)
-    py, ldy, ty = _matrix(y, "y", rows, dim)
-    q, e = _packed(packed, "packed", rows, dim)
-    _rc(lib.het_layer_norm(px, tx, ldx, _vector(gamma, "gamma", dim), _vector(beta, "beta", dim), py, ty, ldy, _vector(mean, "mean", rows),
-                           _vector(rstd, "rstd", rows), q, e, rows, dim, eps, _stream(stream)), "het_layer_norm")
+    dev = _here(x, "x")
+    px, ldx, tx = _matrix(x, "x", rows, dim, dev)
+    py, ldy, ty = _matrix(y, "y", rows, dim, dev)
+    q, e = _packed(packed, "packed", rows, dim, dev)
+    _rc(lib.het_layer_norm(px, tx, ldx, _vector(gamma, "gamma", dim, dev), _vector(beta, "beta", dim, dev), py, ty, ldy,
+                           _vector(mean, "mean", rows, dev), _vector(rstd, "rstd", rows, dev), q, e, rows, dim, eps, _stream(stream, dev)),
+        "het_layer_norm")
 
 
+@functools.lru_cache(maxsize=4096)
 def layer_norm_workspace(rows, dim):
     """Bytes of workspace layer_norm_backward takes."""
     return (_lib or load()).het_layer_norm_workspace(rows, dim)
@@ -177,41 +202,56 @@ def layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, r
     mean is not looked at).  residual: a gradient added to dx."""
     lib = _lib or load()
     rows, dim = _shape(dy, "dy")
-    pdy, lddy, ty = _matrix(dy, "dy", rows, dim)
-    pdx, lddx, tx = _matrix(dx, "dx", rows, dim)
-    kept = isinstance(x, Packed)
-    px, ldx = (None, 0) if kept else _matrix(x, "x", rows, dim, dx.dtype)[:2]
-    q, e = _packed(x if kept else None, "x", rows, dim)
-    pr, ldr = (None, 0) if residual is None else _matrix(residual, "residual", rows, dim, dx.dtype)[:2]
-    if rows and (rstd is None or (not kept and mean is None)):
+    dev = _here(dy, "dy")
+    pdy, lddy, ty = _matrix(dy, "dy", rows, dim, dev)
+    pdx, lddx, tx = _matrix(dx, "dx", rows, dim, dev)
+    px = q = e = pm = pr = None
+    ldx = ldr = 0
+    if isinstance(x, Packed):
+        q, e = _packed(x, "x", rows, dim, dev)
+    else:
+        px, ldx, _ = _matrix(x, "x", rows, dim, dev, dx.dtype)
+        pm = _vector(mean, "mean", rows, dev)
+    if residual is not None:
+        pr, ldr, _ = _matrix(residual, "residual", rows, dim, dev, dx.dtype)
+    if rows and (rstd is None or (px is not None and pm is None)):
         raise ValueError("rstd (and mean, with x itself) must be what layer_norm gave")
-    keep, ws, have = _scratch(lib.het_layer_norm_workspace(rows, dim), workspace, stream)
-    _rc(lib.het_layer_norm_backward(pdy, ty, lddy, px, tx, ldx, None if kept else _vector(mean, "mean", rows), _vector(rstd, "rstd", rows), q, e,
-                                    _vector(gamma, "gamma", dim), pr, ldr, pdx, lddx, _vector(dgamma, "dgamma", dim),
-                                    _vector(dbeta, "dbeta", dim), rows, dim, ws, have, _stream(stream)), "het_layer_norm_backward")
+    keep, ws, have = _scratch(layer_norm_workspace(rows, dim), workspace, stream, dev)
+    _rc(lib.het_layer_norm_backward(pdy, ty, lddy, px, tx, ldx, pm, _vector(rstd, "rstd", rows, dev), q, e, _vector(gamma, "gamma", dim, dev), pr, ldr, pdx, lddx,
+                                    _vector(dgamma, "dgamma", dim, dev), _vector(dbeta, "dbeta", dim, dev), rows, dim, ws, have, _stream(stream, dev)),
+        "het_layer_norm_backward")
 
 
 def pack(x, packed, stream=None):
     """x in 8 bits into `packed` (het_pack)."""
     lib = _lib or load()
     rows, dim = _shape(x, "x")
-    px, ldx, tx = _matrix(x, "x", rows, dim)
-    q, e = _packed(packed, "packed", rows, dim)
-    _rc(lib.het_pack(px, tx, ldx, q, e, rows, dim, _stream(stream)), "het_pack")
+    dev = _here(x, "x")
+    px, ldx, tx = _matrix(x, "x", rows, dim, dev)
+    q, e = _packed(packed, "packed", rows, dim, dev)
+    _rc(lib.het_pack(px, tx, ldx, q, e, rows, dim, _stream(stream, dev)), "het_pack")
 
 
 def expand(packed, y, act=ACT_NONE, gamma=None, beta=None, stream=None):
     """y = act(gamma v + beta) of the values v that `packed` holds (het_expand)."""
     lib = _lib or load()
     rows, dim = _shape(packed, "packed")
-    py, ldy, ty = _matrix(y, "y", rows, dim)
-    q, e = _packed(packed, "packed", rows, dim)
-    _rc(lib.het_expand(q, e, rows, dim, _vector(gamma, "gamma", dim), _vector(beta, "beta", dim), act, py, ty, ldy, _stream(stream)), "het_expand")
+    dev = _here(packed, "packed")
+    py, ldy, ty = _matrix(y, "y", rows, dim, dev)
+    q, e = _packed(packed, "packed", rows, dim, dev)
+    _rc(lib.het_expand(q, e, rows, dim, _vector(gamma, "gamma", dim, dev), _vector(beta, "beta", dim, dev), act, py, ty, ldy, _stream(stream, dev)), "het_expand")
 
 
-def _run_linear(lib, l, call, what, backward, workspace, stream):
-    keep, l.workspace, l.workspace_bytes = _scratch(lib.het_linear_workspace(C.byref(l), backward), workspace, stream)
-    _rc(call(C.byref(l), _stream(stream)), what)
+@functools.lru_cache(maxsize=4096)
+def _linear_workspace(rows, inp, out, kind, backward, xq, dx, dw, dbias):
+    l = linear_struct(rows=rows, inp=inp, out=out, type=kind, xq=xq, dx=dx, dw=dw, dbias=dbias)
+    return (_lib or load()).het_linear_workspace(l, backward)
+
+
+def linear_workspace(rows, inp, out, dtype, backward=False, x_packed=False, dx=True, dw=True, dbias=True):
+    """Bytes of workspace linear or linear_backward takes; x_packed: x is kept in 8 bits; dx, dw, dbias: which of them are wanted."""
+    load()
+    return _linear_workspace(rows, inp, out, _types[dtype], int(backward), int(x_packed), int(dx), int(dw), int(dbias))
 
 
 def linear(x, w, bias, y, act=ACT_NONE, residual=None, z=None, workspace=None, stream=None):
@@ -220,18 +260,21 @@ def linear(x, w, bias, y, act=ACT_NONE, residual=None, z=None, workspace=None, s
     lib = _lib or load()
     rows, inp = _shape(x, "x")
     out = _shape(w, "w")[0]
-    l = Linear(rows=rows, inp=inp, out=out, act=act)
-    l.x, l.ldx, l.type = _matrix(x, "x", rows, inp)
-    l.w, l.ldw, _ = _matrix(w, "w", out, inp, x.dtype)
-    l.bias = _vector(bias, "bias", out)
-    l.y, l.ldy, l.y_type = _matrix(y, "y", rows, out)
+    dev = _here(x, "x")
+    px, ldx, kind = _matrix(x, "x", rows, inp, dev)
+    pw, ldw, _ = _matrix(w, "w", out, inp, dev, x.dtype)
+    py, ldy, y_kind = _matrix(y, "y", rows, out, dev)
+    pr = pz = zq = ze = None
+    ldr = ldz = 0
     if residual is not None:
-        l.residual, l.ld_residual, _ = _matrix(residual, "residual", rows, out, y.dtype)
+        pr, ldr, _ = _matrix(residual, "residual", rows, out, dev, y.dtype)
     if isinstance(z, Packed):
-        l.zq, l.ze = _packed(z, "z", rows, out)
+        zq, ze = _packed(z, "z", rows, out, dev)
     elif z is not None:
-        l.z, l.ldz, _ = _matrix(z, "z", rows, out, x.dtype)
-    _run_linear(lib, l, lib.het_linear, "het_linear", 0, workspace, stream)
+        pz, ldz, _ = _matrix(z, "z", rows, out, dev, x.dtype)
+    keep, ws, have = _scratch(_linear_workspace(rows, inp, out, kind, 0, 0, 0, 0, 0), workspace, stream, dev)
+    _rc(lib.het_linear(_linear_t.pack(rows, inp, out, kind, y_kind, act, 0, px, ldx, 0, 0, 0, 0, pw, ldw, _vector(bias, "bias", out, dev) or 0, pr or 0, ldr, py, ldy,
+                                      pz or 0, ldz, zq or 0, ze or 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, ws or 0, have), _stream(stream, dev)), "het_linear")
 
 
 def linear_backward(dy, x, w, z, act, dz, dx, dw, dbias=None, x_act=ACT_NONE, x_gamma=None, x_beta=None, workspace=None, stream=None):
@@ -243,40 +286,38 @@ def linear_backward(dy, x, w, z, act, dz, dx, dw, dbias=None, x_act=ACT_NONE, x_
     if ref is None:
         raise ValueError("w or dw says how wide the layer's input is")
     inp, dtype = _shape(ref, "w")[1], ref.dtype
-    l = Linear(rows=rows, inp=inp, out=out, act=act, x_act=x_act)
-    if dtype not in _types:
+    kind = _types.get(dtype)
+    if kind is None:
         raise TypeError("w must be float32, bfloat16 or float16")
-    l.type = _types[dtype]
-    l.dy, l.lddy, l.y_type = _matrix(dy, "dy", rows, out)
+    dev = _here(dy, "dy")
+    pdy, lddy, y_kind = _matrix(dy, "dy", rows, out, dev)
+    px = pxq = pxe = pg = pb = pw = pz = pzq = pze = pdz = pdx = pdw = None
+    ldx = ldw = ldz = lddz = lddx = lddw = 0
     if dz is not None:
-        l.dz, l.lddz, _ = _matrix(dz, "dz", rows, out, dtype)
+        pdz, lddz, _ = _matrix(dz, "dz", rows, out, dev, dtype)
     if isinstance(z, Packed):
-        l.zq, l.ze = _packed(z, "z", rows, out)
+        pzq, pze = _packed(z, "z", rows, out, dev)
     elif z is not None:
-        l.z, l.ldz, _ = _matrix(z, "z", rows, out, dtype)
+        pz, ldz, _ = _matrix(z, "z", rows, out, dev, dtype)
     if dx is not None:
         if w is None:
             raise ValueError("dx needs w")
-        l.dx, l.lddx, _ = _matrix(dx, "dx", rows, inp, dtype)
-        l.w, l.ldw, _ = _matrix(w, "w", out, inp, dtype)
+        pdx, lddx, _ = _matrix(dx, "dx", rows, inp, dev, dtype)
+        pw, ldw, _ = _matrix(w, "w", out, inp, dev, dtype)
     if dw is not None:
-        l.dw, l.lddw, _ = _matrix(dw, "dw", out, inp, dtype)
+        pdw, lddw, _ = _matrix(dw, "dw", out, inp, dev, dtype)
         if isinstance(x, Packed):
-            l.xq, l.xe = _packed(x, "x", rows, inp)
-            l.x_gamma, l.x_beta = _vector(x_gamma, "x_gamma", inp), _vector(x_beta, "x_beta", inp)
+            pxq, pxe = _packed(x, "x", rows, inp, dev)
+            pg, pb = _vector(x_gamma, "x_gamma", inp, dev), _vector(x_beta, "x_beta", inp, dev)
         elif x is None:
             raise ValueError("dw needs x")
         else:
-            l.x, l.ldx, _ = _matrix(x, "x", rows, inp, dtype)
+            px, ldx, _ = _matrix(x, "x", rows, inp, dev, dtype)
             if x_act != ACT_NONE or x_gamma is not None or x_beta is not None:
                 raise ValueError("x_act, x_gamma and x_beta are for an x kept in 8 bits")
-    l.dbias = _vector(dbias, "dbias", out)
-    _run_linear(lib, l, lib.het_linear_backward, "het_linear_backward", 1, workspace, stream)
-
-
-def linear_workspace(rows, inp, out, dtype, backward=False, x_packed=False, dx=True, dw=True, dbias=True):
-    """Bytes of workspace linear or linear_backward takes; x_packed: x is kept in 8 bits; dx, dw, dbias: which of them are wanted."""
-    lib = _lib or load()
-    l = Linear(rows=rows, inp=inp, out=out, type=_types[dtype], xq=1 if x_packed else None, dx=1 if dx else None, dw=1 if dw else None,
-               dbias=1 if dbias else None)
-    return lib.het_linear_workspace(C.byref(l), 1 if backward else 0)
+    pdb = _vector(dbias, "dbias", out, dev)
+    need = _linear_workspace(rows, inp, out, kind, 1, int(bool(pxq)), int(bool(pdx)), int(bool(pdw)), int(bool(pdb)))
+    keep, ws, have = _scratch(need, workspace, stream, dev)
+    _rc(lib.het_linear_backward(_linear_t.pack(rows, inp, out, kind, y_kind, act, x_act, px or 0, ldx, pxq or 0, pxe or 0, pg or 0, pb or 0, pw or 0, ldw, 0, 0, 0, 0, 0,
+                                               pz or 0, ldz, pzq or 0, pze or 0, pdy, lddy, pdz or 0, lddz, pdx or 0, lddx, pdw or 0, lddw, pdb or 0, ws or 0, have),
+                                _stream(stream, dev)), "het_linear_backward")

@@ -26,7 +26,7 @@ def test_the_struct_is_the_headers():
     text = open(os.path.join(ROOT, "include", "het_dense.h")).read()
     body = re.sub(r"/\*.*?\*/", "", re.search(r"typedef struct het_linear_t \{(.*?)\} het_linear_t;", text, re.S).group(1), flags=re.S)
     names = [n.strip(" *") for line in body.split(";") if line.strip() for n in re.sub(r"^\s*(const\s+)?\w+", "", line).split(",")]
-    assert [{"in": "inp"}.get(n, n) for n in names] == [n for n, _ in dense.Linear._fields_]
+    assert [{"in": "inp"}.get(n, n) for n in names] == list(dense.LINEAR_FIELDS)
 
 
 def norm(lib, **kw):
@@ -71,7 +71,7 @@ def linear_args(**kw):
     a = dict(rows=300, inp=256, out=128, type=1, y_type=1, act=2, x=P, ldx=256, w=P, ldw=256, bias=P, y=P, ldy=128, dy=P, lddy=128, dz=P, lddz=128, dx=P, lddx=256,
              dw=P, lddw=256, dbias=P, zq=P, ze=P, workspace=P, workspace_bytes=1 << 30)
     a.update(kw)
-    return dense.Linear(**a)
+    return dense.linear_struct(**a)
 
 
 COMMON = [dict(rows=-1), dict(rows=(1 << 31) - 1), dict(inp=0), dict(out=0), dict(inp=(1 << 20) + 1, ldx=1 << 21, ldw=1 << 21), dict(type=3), dict(type=0, y_type=1),
@@ -81,7 +81,7 @@ COMMON = [dict(rows=-1), dict(rows=(1 << 31) - 1), dict(inp=0), dict(out=0), dic
 @pytest.mark.parametrize("bad", COMMON + [dict(x=None), dict(w=None), dict(y=None), dict(ldx=255), dict(ldy=127), dict(residual=P, ld_residual=127), dict(z=P, ldz=127),
                                           dict(zq=P + 8), dict(zq=None)])
 def test_linear_refuses(bad):
-    assert dense.load().het_linear(C.byref(linear_args(**bad)), None) == HET_EINVAL
+    assert dense.load().het_linear(linear_args(**bad), None) == HET_EINVAL
 
 
 @pytest.mark.parametrize("bad", COMMON + [dict(dy=None), dict(dz=None), dict(zq=None), dict(zq=None, ze=None), dict(zq=None, ze=None, z=P, ldz=127), dict(w=None),
@@ -89,7 +89,7 @@ def test_linear_refuses(bad):
                                           dict(xq=P + 8, xe=P), dict(x_act=9), dict(dz=None, act=0, y_type=0), dict(workspace=None), dict(workspace=P + 4),
                                           dict(workspace_bytes=0)])
 def test_linear_backward_refuses(bad):
-    assert dense.load().het_linear_backward(C.byref(linear_args(**bad)), None) == HET_EINVAL
+    assert dense.load().het_linear_backward(linear_args(**bad), None) == HET_EINVAL
 
 
 def test_a_null_layer_is_refused():
@@ -102,7 +102,7 @@ def test_calls_without_rows_have_nothing_to_do():
     assert norm(lib, rows=0, x=None, y=None) == HET_OK
     assert lib.het_pack(None, 1, 40, None, None, 0, 40, None) == HET_OK
     assert lib.het_expand(None, None, 0, 40, None, None, 0, None, 1, 40, None) == HET_OK
-    assert lib.het_linear(C.byref(linear_args(rows=0, x=None, y=None, zq=None, ze=None)), None) == HET_OK
+    assert lib.het_linear(linear_args(rows=0, x=None, y=None, zq=None, ze=None), None) == HET_OK
     assert back(lib, rows=0, dy=None, x=None, dx=None, mean=None, rstd=None, dgamma=None, dbeta=None) == HET_OK
 
 
@@ -113,7 +113,7 @@ def test_a_workspace_of_the_size_that_is_named_is_needed():
         assert need > 0
         l = linear_args(rows=rows, inp=inp, out=out, type=dense.load() and dense._types[dtype], y_type=dense._types[dtype], ldx=inp, ldw=inp, lddx=inp, lddw=inp, lddy=out,
                         lddz=out, ldy=out, workspace_bytes=need - 1)
-        assert lib.het_linear_backward(C.byref(l), None) == HET_EINVAL
+        assert lib.het_linear_backward(l, None) == HET_EINVAL
     assert dense.linear_workspace(-1, 8, 8, torch.float32) == HET_EINVAL
     assert dense.layer_norm_workspace(4, 0) == HET_EINVAL
 

@@ -393,7 +393,8 @@ def test_expand_through_weights_and_activation(rows, dim, affine, act, t):
 # (rows, in, out): single tokens and the sizes at which the kernel for few rows gives way; edges of a tile (128, 32), of a step (32, 64) and of a piece; long
 # sums over few tiles (split); widths of one
 LINEAR_SHAPES = [(1, 1, 1), (1, 64, 16), (1, 1664, 33), (2, 7, 5), (8, 130, 40), (16, 64, 32), (17, 96, 31), (33, 200, 65), (64, 72, 48), (65, 64, 128), (100, 33, 17),
-                 (128, 128, 128), (129, 65, 127), (200, 31, 260), (130, 640, 129), (257, 1001, 70), (66, 3000, 130), (384, 192, 256), (300, 8, 300), (520, 320, 264)]
+                 (128, 128, 128), (129, 65, 127), (200, 31, 260), (130, 640, 129), (257, 1001, 70), (66, 3000, 130), (384, 192, 256), (300, 8, 300), (520, 320, 264),
+                 (700, 2000, 640), (640, 4200, 1030)]
 LINEAR_TYPES = [(F32, F32), (BF16, BF16), (F16, F16), (BF16, F32), (F16, F32)]
 
 
@@ -477,8 +478,8 @@ def test_linear_backward(rows, inp, out, t, ty, kept):
         assert torch.equal(again, dw.m), "one output alone: the same bits"
     if t == ty:                                                 # no activation: dz is dy, written into itself or not at all
         a, b = torch.empty(rows, inp, dtype=t, device="cuda"), torch.empty(rows, inp, dtype=t, device="cuda")
-        dense.linear_backward(dy, None, w, None, dense.ACT_NONE, None, a, None)
-        same = dy.clone()
+        same = dy.clone()                                       # (how an operand lies decides how its sums are divided: the same in both calls)
+        dense.linear_backward(same, None, w, None, dense.ACT_NONE, None, a, None)
         dense.linear_backward(same, None, w, None, dense.ACT_NONE, same, b, None, db)
         assert torch.equal(a, b) and torch.equal(same, dy)
 
@@ -557,13 +558,13 @@ def test_a_layer_of_no_input_rows_beyond_and_offsets_past_32_bits():
 
 
 def test_a_workspace_that_is_too_small_is_refused():
-    x, w, y = torch.zeros(70, 4000, device="cuda"), torch.zeros(30, 4000, device="cuda"), torch.zeros(70, 30, device="cuda")
-    need = dense.linear_workspace(70, 4000, 30, F32)
+    x, w, y = torch.zeros(1000, 16384, device="cuda"), torch.zeros(300, 16384, device="cuda"), torch.zeros(1000, 300, device="cuda")
+    need = dense.linear_workspace(1000, 16384, 300, F32)                # a long sum over few tiles is split
     assert need > 16
     with pytest.raises(HetError):
         dense.linear(x, w, None, y, workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
     dense.linear(x, w, None, y, workspace=torch.empty(need, dtype=torch.uint8, device="cuda"))
-    v = torch.zeros(70, device="cuda")
+    v = torch.zeros(1000, device="cuda")
     with pytest.raises(HetError):
         dense.layer_norm_backward(y, y, None, v, v, y, workspace=torch.empty(8, dtype=torch.uint8, device="cuda"))
 
