@@ -317,6 +317,7 @@ struct SlopeArgs {
 };
 
 constexpr int SLOPE_COLS = 32 * CHUNK;
+constexpr int SLOPE_ROWS = 2;              // rows a thread has in flight
 
 template <typename T, typename TY, bool WHOLE>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
@@ -325,24 +326,37 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     const int cx = threadIdx.x % 32, ry = threadIdx.x / 32, c = blockIdx.x * 32 + cx, n = chunk_values(c, a.dim);
     f32x8 s = {};
     if (n > 0)
-        for (int64_t row = (int64_t)blockIdx.y * 8 + ry; row < a.rows; row += 8 * (int64_t)gridDim.y) {
-            f32x8 d = load_row<WHOLE>(static_cast<const TY *>(a.dy) + row * a.lddy, c, a.dim);
-            if (a.act != DENSE_ACT_NONE) {
-                f32x8 z;
+        for (int64_t row = (int64_t)blockIdx.y * 8 + ry; row < a.rows; row += SLOPE_ROWS * 8 * (int64_t)gridDim.y) {
+            vec<TY, 8> dy[SLOPE_ROWS];
+            vec<T, 8> z[SLOPE_ROWS];
+            uint64_t q[SLOPE_ROWS];
+            uint8_t e[SLOPE_ROWS];
+#pragma unroll
+            for (int u = 0; u < SLOPE_ROWS; ++u) {
+                const int64_t at = row + u * 8 * (int64_t)gridDim.y, in = at < a.rows ? at : row;
+                dy[u] = load_raw<WHOLE>(static_cast<const TY *>(a.dy) + in * a.lddy, c, a.dim);
+                if (a.act == DENSE_ACT_NONE) continue;
                 if (a.q) {
-                    uint64_t q;
-                    __builtin_memcpy(&q, a.q + row * a.pitch + c * CHUNK, 8);
-                    z = unpack_chunk(q, a.e[row * (a.pitch / PACK_BLOCK) + (c >> 2)]);
+                    __builtin_memcpy(&q[u], a.q + in * a.pitch + c * CHUNK, 8);
+                    e[u] = a.e[in * (a.pitch / PACK_BLOCK) + (c >> 2)];
                 } else {
-                    z = load_row<WHOLE>(static_cast<const T *>(a.z) + row * a.ldz, c, a.dim);
+                    z[u] = load_raw<WHOLE>(static_cast<const T *>(a.z) + in * a.ldz, c, a.dim);
                 }
-                z = act_chunk<true>(a.act, z);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d[j] *= z[j];
             }
-            if (a.dz) store_row<WHOLE>(static_cast<T *>(a.dz) + row * a.lddz, c, a.dim, d);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] += (WHOLE || j < n) ? d[j] : 0.f;
+            for (int u = 0; u < SLOPE_ROWS; ++u) {
+                const int64_t at = row + u * 8 * (int64_t)gridDim.y;
+                if (at >= a.rows) break;
+                f32x8 d = raw_values<WHOLE>(dy[u], c, a.dim);
+                if (a.act != DENSE_ACT_NONE) {
+                    const f32x8 slope = act_chunk<true>(a.act, a.q ? unpack_chunk(q[u], e[u]) : raw_values<WHOLE>(z[u], c, a.dim));
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d[j] *= slope[j];
+                }
+                if (a.dz) store_row<WHOLE>(static_cast<T *>(a.dz) + at * a.lddz, c, a.dim, d);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j] += (WHOLE || j < n) ? d[j] : 0.f;
+            }
         }
     if (!a.partial) return;
 #pragma unroll

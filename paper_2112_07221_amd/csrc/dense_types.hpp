@@ -101,23 +101,30 @@ enum { DENSE_ACT_NONE = 0, DENSE_ACT_RELU = 1, DENSE_ACT_GELU = 2, DENSE_ACT_SIL
 
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * 1.4426950408889634f); }
 
-// Phi(-|v|), the normal distribution's smaller tail, and exp(-v^2 / 2), of which it is a multiple: erfc by the rational approximation 7.1.26 of
-// Abramowitz and Stegun (Handbook of Mathematical Functions), off by at most 1.5e-7, half of that here.  The tail is formed itself, not as
-// 1 - erf, so no digits are lost for negative v.  One exponential and one reciprocal for value and slope alike: with the math library's
-// erf and exp slope_kernel took 58.2 us for 8192 x 4096 values (bf16, z in 8 bits), 40.0 with this; memory's share is 33.
-__device__ __forceinline__ float normal_tail(float v, float &bell)
+// Phi(-|v|), the normal distribution's smaller tail.  Its logarithm is -v^2 / 2 and a slow function of |v|, for which stands a polynomial of degree
+// 6 (a least-squares fit of log2(Phi(-x)) + x^2 / 2 log2(e) on [0, 7], weighted by what an error does to x Phi(-x); beyond 7 the tail is below 2e-12
+// and the polynomial stays where it is): Phi is off by at most 3.2e-7, v Phi(v) by 2.1e-7.  The tail is formed itself, not as 1 - erf, so no digits are
+// lost for negative v.  One exponential, six multiply-adds: with the math library's erf and exp slope_kernel took 58.2 us for 8192 x 4096 values
+// (bf16, z in 8 bits; memory's share is 33), with the rational approximation 7.1.26 of Abramowitz and Stegun 40.0.
+__device__ __forceinline__ float normal_exponent(float v) { return v * -0.72134752044448170f * v; }        // log2 exp(-v^2 / 2)
+__device__ __forceinline__ float normal_tail(float v)
 {
-    bell = exp_of(-0.5f * v * v);
-    const float t = __builtin_amdgcn_rcpf(1.f + 0.3275911f * 0.70710678118654752f * fabsf(v));
-    return 0.5f * t * bell * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    const float x = fminf(fabsf(v), 7.f);
+    float q = 2.8578077035490423e-05f;
+    q = fmaf(q, x, -0.0007268775952979922f);
+    q = fmaf(q, x, 0.007932470180094242f);
+    q = fmaf(q, x, -0.053169168531894684f);
+    q = fmaf(q, x, 0.26238641142845154f);
+    q = fmaf(q, x, -1.151138186454773f);
+    q = fmaf(q, x, -0.9999993443489075f);
+    return __builtin_amdgcn_exp2f(normal_exponent(v) + q);
 }
 
 __device__ __forceinline__ float act_value(int act, float v)
 {
-    float bell;
     switch (act) {
     case DENSE_ACT_RELU: return v > 0.f ? v : v == v ? 0.f : v;                       // NaN stays NaN
-    case DENSE_ACT_GELU: { const float tail = normal_tail(v, bell); return v * (v < 0.f ? tail : 1.f - tail); }
+    case DENSE_ACT_GELU: { const float tail = normal_tail(v); return v * (v < 0.f ? tail : 1.f - tail); }
     case DENSE_ACT_SILU: return v * __builtin_amdgcn_rcpf(1.f + exp_of(-v));
     default: return v;
     }
@@ -125,10 +132,12 @@ __device__ __forceinline__ float act_value(int act, float v)
 
 __device__ __forceinline__ float act_slope(int act, float v)
 {
-    float bell;
     switch (act) {
     case DENSE_ACT_RELU: return v > 0.f ? 1.f : v == v ? 0.f : v;
-    case DENSE_ACT_GELU: { const float tail = normal_tail(v, bell); return (v < 0.f ? tail : 1.f - tail) + v * (0.39894228040143268f * bell); }
+    case DENSE_ACT_GELU: {
+        const float tail = normal_tail(v);
+        return fmaf(v * 0.39894228040143268f, __builtin_amdgcn_exp2f(normal_exponent(v)), v < 0.f ? tail : 1.f - tail);
+    }
     case DENSE_ACT_SILU: { const float p = __builtin_amdgcn_rcpf(1.f + exp_of(-v)); return p * (1.f + v * (1.f - p)); }
     default: return 1.f;
     }
@@ -161,8 +170,8 @@ __device__ __forceinline__ uint32_t magnitude(float v) { return __float_as_uint(
 
 struct PackStep {
     uint32_t byte;       // what is stored
+    uint32_t finite;     // all ones, or zero
     float inverse;       // 2^-e
-    float most;          // largest number of steps
 };
 
 // most_bits: magnitude() of the block's largest value.  A significand of 127.5 / 64 and above rounds to 128 steps: adding 2^16 (its distance
@@ -172,23 +181,24 @@ __device__ __forceinline__ PackStep pack_step(uint32_t most_bits)
     PackStep s;
     int e = (int)((most_bits + 0x10000u) >> 23) - 133;
     e = e < -126 ? -126 : e > 122 ? 122 : e;
-    s.byte = most_bits >= 0x7F800000u ? PACK_NOT_FINITE : (uint32_t)(e + 127);
-    s.inverse = most_bits >= 0x7F800000u ? 0.f : __uint_as_float((uint32_t)(127 - e) << 23);
-    s.most = e == 122 ? 63.f : 127.f;       // 64 steps of 2^122 would be no float any more
+    s.finite = most_bits < 0x7F800000u ? ~0u : 0u;
+    s.byte = s.finite ? (uint32_t)(e + 127) : PACK_NOT_FINITE;
+    s.inverse = __uint_as_float((uint32_t)(127 - e) << 23);
     return s;
 }
 
-__device__ __forceinline__ int pack_value(float v, const PackStep &s)
-{
-    if (s.byte == PACK_NOT_FINITE) return 0;
-    const float q = __builtin_rintf(v * s.inverse);
-    return (int)(q > s.most ? s.most : q < -s.most ? -s.most : q);
-}
-
+// Four values as bytes.  Adding 3 2^22 leaves the whole number, rounded to even, in the float's low bits: one multiply-add a value and three byte
+// permutations for four.  The step is such that no value is beyond 127 of it; at the top of the range alone it is held below 64
+// (64 steps of 2^122 would be no float any more).
 __device__ __forceinline__ uint32_t pack_four(float a, float b, float c, float d, const PackStep &s)
 {
-    return ((uint32_t)pack_value(a, s) & 255u) | ((uint32_t)pack_value(b, s) & 255u) << 8 | ((uint32_t)pack_value(c, s) & 255u) << 16 |
-           (uint32_t)pack_value(d, s) << 24;
+    if (s.byte == 249u) {
+        const float most = 63.f / s.inverse;
+        a = fminf(fmaxf(a, -most), most); b = fminf(fmaxf(b, -most), most); c = fminf(fmaxf(c, -most), most); d = fminf(fmaxf(d, -most), most);
+    }
+    const uint32_t p = __float_as_uint(fmaf(a, s.inverse, 12582912.f)), q = __float_as_uint(fmaf(b, s.inverse, 12582912.f));
+    const uint32_t r = __float_as_uint(fmaf(c, s.inverse, 12582912.f)), t = __float_as_uint(fmaf(d, s.inverse, 12582912.f));
+    return (__builtin_amdgcn_perm(q, p, 0x0C0C0400u) | __builtin_amdgcn_perm(t, r, 0x04000C0Cu)) & s.finite;
 }
 
 // 2^e of a stored byte; 255 gives infinity, and 0 times that the NaN the block stands for.
