@@ -39,7 +39,7 @@ void launch_column_sum(const float *partial, int n, int sets, int dim, float *ou
     ColumnSumArgs s;
     s.partial = partial; s.out[0] = out0; s.out[1] = out1;
     s.n = n; s.sets = sets; s.width = width_of(dim); s.dim = dim;
-    column_sum_kernel<<<(uint32_t)cdiv((int64_t)sets * s.width, 16), 256, 0, st>>>(s);
+    column_sum_kernel<<<(uint32_t)cdiv((int64_t)sets * s.width, 16), COLUMN_THREADS, 0, st>>>(s);
 }
 
 // f(tag of x's type, tag of y's type); false: no such pair.
@@ -86,8 +86,8 @@ void launch_slope(const SlopeArgs &s, dim3 grid, hipStream_t st)
 
 int slope_splits(int64_t rows, int32_t out)
 {
-    // enough workgroups to fill the chip, at least 32 rows for each
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)PARTIALS, cdiv(rows, 32), cdiv(2048, cdiv(out, SLOPE_COLS))}));
+    // enough workgroups to fill the chip, a turn of rows for each at least
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)PARTIALS, cdiv(rows, 8 * SLOPE_ROWS), cdiv(2048, cdiv(out, SLOPE_COLS))}));
 }
 
 struct BackPlan {

@@ -492,11 +492,24 @@ struct Direct {
             for (int j = 0; j < PIECE; ++j) f[j] = p[(k + j) * ld];
         return f;
     }
-    __device__ __forceinline__ F load_edge(int k, int end) const      // zero from `end` on
+    // Zero from `end` on.  No lane takes a branch of its own: a piece that would cross the end is the last one before it, shifted.
+    __device__ __forceinline__ F load_edge(int k, int end) const
     {
+        if (K && end >= PIECE) {
+            const int from = k < end - PIECE ? k : end - PIECE, over = k - from;
+            unsigned __int128 v;
+            __builtin_memcpy(&v, p + from, 16);
+            v = over < PIECE ? v >> (8 * (int)sizeof(T) * over) : 0;
+            return __builtin_bit_cast(F, v);
+        }
         F f;
 #pragma unroll
-        for (int j = 0; j < PIECE; ++j) f[j] = k + j < end ? p[K ? (int64_t)(k + j) : (k + j) * ld] : (T)0.f;
+        for (int j = 0; j < PIECE; ++j) {
+            const int at = k + j < end ? k + j : end - 1;
+            f[j] = p[K ? (int64_t)at : at * ld];
+        }
+#pragma unroll
+        for (int j = 0; j < PIECE; ++j) f[j] = k + j < end ? f[j] : (T)0.f;
         return f;
     }
 };

@@ -269,36 +269,38 @@ __global__ __launch_bounds__(MOST) void norm_back_kernel(NormBackArgs a)
     }
 }
 
-// Column sums of partial[n][sets][width]: set s goes to out[s] (null: nobody asks).  16 columns a workgroup, 16 threads for each of them, which
-// take every 16th row; their sums are added in order.
+// Column sums of partial[n][sets][width]: set s goes to out[s] (null: nobody asks).  16 columns a workgroup, 64 threads for each of them, which
+// take every 64th row, eight of them in flight: 512 rows are one turn.  The threads' sums are added in order.
 struct ColumnSumArgs {
     const float *partial;
     float *out[2];
     int n, sets, width, dim;
 };
 
-static __global__ __launch_bounds__(256) void column_sum_kernel(ColumnSumArgs a)
+constexpr int COLUMN_THREADS = 1024;
+
+static __global__ __launch_bounds__(COLUMN_THREADS) void column_sum_kernel(ColumnSumArgs a)
 {
-    __shared__ float lds[16][17];
+    constexpr int DEEP = COLUMN_THREADS / 16;
+    __shared__ float lds[DEEP][17];
     const int cx = threadIdx.x % 16, ry = threadIdx.x / 16, col = blockIdx.x * 16 + cx, total = a.sets * a.width;
+    const float *p = a.partial + (col < total ? col : 0);
     float s = 0.f;
-    if (col < total) {
-        const float *p = a.partial + col;
-        int r = ry;
-        for (; r + 7 * 16 < a.n; r += 8 * 16) {
-            float v[8];
+    for (int r = ry; r < a.n; r += 8 * DEEP) {
+        float v[8];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) v[u] = p[(size_t)(r + u * 16) * total];
+        for (int u = 0; u < 8; ++u) v[u] = p[(size_t)(r + u * DEEP < a.n ? r + u * DEEP : r) * total];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) s += v[u];
-        }
-        for (; r < a.n; r += 16) s += p[(size_t)r * total];
+        for (int u = 0; u < 8; ++u) s += r + u * DEEP < a.n ? v[u] : 0.f;
     }
     lds[ry][cx] = s;
     __syncthreads();
-    if (ry || col >= total) return;
+    if (ry >= 4) return;                                  // four threads a column, then one
 #pragma unroll
-    for (int u = 1; u < 16; ++u) s += lds[u][cx];
+    for (int u = 1; u < DEEP / 4; ++u) s += lds[ry + 4 * u][cx];
+    s += __shfl_xor(s, 16);
+    s += __shfl_xor(s, 32);
+    if (ry || col >= total) return;
     const int set = col / a.width, at = col % a.width;
     if (at < a.dim && a.out[set]) a.out[set][at] = s;
 }
