@@ -197,6 +197,72 @@ def pattern_study(args, w, dev):
                       "dim": D, "slots": P, "build_id": hc.build_id(), "rows": rows}))
 
 
+def dense_step(args, w, dev):
+    """A whole training step: lookup, a residual block over each sample's rows (dense.ResidualBlock: layer norm, two linear layers, activations kept in 8
+    bits), the block's backward pass, update of the rows, plain SGD on the block's weights.  Its loss is half the squared distance to fixed
+    targets.  One JSON line: milliseconds of the whole step, of the cache's part alone and of the block's two passes alone."""
+    import torch
+    from paper_2112_07221_amd import dense
+    from paper_2112_07221_amd import hetcache as hc
+    from paper_2112_07221_amd import workloads as wl
+    W, K = args.warmup, args.steps
+    ids = torch.from_numpy(wl.IdStream(w).batches(W + K)).to(dev)
+    offsets = torch.from_numpy(wl.bag_offsets(w)).to(dev) if w.pooled else None
+    rows, wide = (w.batch, w.dim) if w.pooled else (w.batch, w.width * w.dim)
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(wl.seeds(w.index)["grads"])
+    block = dense.ResidualBlock(rows, wide, args.hidden, torch.bfloat16, generator=gen)
+    x, y, dx, target = (torch.randn(rows, wide, generator=gen, device=dev) for _ in range(4))
+
+    def run(with_cache, with_block):
+        Wt = torch.from_numpy(wl.table_init(w)).to(dev)
+        cache = hc.HetCache(w.capacity, w.dim, w.s, w.policy, w.n, w.optimizer, w.eps)
+        cache.attach_backing(Wt, torch.zeros_like(Wt) if w.optimizer else None, torch.zeros(w.vocab, dtype=torch.int32, device=dev), hc.BACKING_HBM)
+
+        def step(t):
+            if with_cache:
+                if t == 0 and W + K > 1:
+                    cache.prefetch(ids[1])
+                if t + 2 < W + K:
+                    cache.prefetch(ids[t + 2])
+                if w.pooled:
+                    cache.lookup_pooled(ids[t], offsets, x)
+                else:
+                    cache.lookup(ids[t], x)
+            if with_block:
+                block.forward(x, y)
+                y.sub_(target)
+                block.backward(y, dx)
+            if with_cache:
+                if w.pooled:
+                    cache.update_pooled(ids[t], offsets, dx, w.lr)
+                else:
+                    cache.update(ids[t], dx, w.lr)
+            if with_cache and with_block:
+                for p, grad in block.parameters():
+                    p.add_(grad, alpha=-1e-6)
+
+        for t in range(W):
+            step(t)
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for t in range(W, W + K):
+            step(t)
+        torch.cuda.synchronize()
+        ms = (time.perf_counter() - t0) * 1e3 / K
+        bits = cache.stats()["error_bits"]
+        cache.close()
+        assert bits == 0, "device error bits set during the run"
+        return ms
+
+    whole, cache_ms, block_ms = run(True, True), run(True, False), run(False, True)
+    flops = 12.0 * rows * wide * args.hidden
+    print(json.dumps({"study": "training step with a residual block between lookup and update", "config": w.index, "rows": rows, "dim": wide,
+                      "hidden": args.hidden, "dtype": "bf16, residual stream f32", "steps": K, "warmup": W, "ms_per_step": whole,
+                      "ms_cache_alone": cache_ms, "ms_block_alone": block_ms, "block_TFLOPs": flops / (block_ms * 1e-3) / 1e12,
+                      "build_id": hc.build_id()}))
+
+
 def trace_kernels(args, w, dev):
     """Where the two heavy kernels' time goes: per-workgroup time stamps (het_profile_trace) of one
     lookup and one update after `--warmup` steps, summarised per role and per phase.  One JSON line."""
@@ -302,6 +368,10 @@ def main():
     ap.add_argument("--pattern-study", action="store_true",
                     help="instead of the benchmark: what plain copy, gather and read-modify-write kernels reach at the "
                          "chosen config's sizes (reference points beside the streaming peak)")
+    ap.add_argument("--dense-step", action="store_true",
+                    help="instead of the benchmark: a whole training step (table in HBM), with a residual block (layer norm, two linear "
+                         "layers, 8-bit activations) between lookup and update")
+    ap.add_argument("--hidden", type=int, default=4096, help="--dense-step: values inside the block")
     args = ap.parse_args()
     if args.gpus != 1:
         print("bench.py: this build runs on one GPU only (no sharding, no collectives); "
@@ -322,6 +392,9 @@ def main():
         return
     if args.trace_kernels:
         trace_kernels(args, w, dev)
+        return
+    if args.dense_step:
+        dense_step(args, w, dev)
         return
     K, W = args.steps, args.warmup
     total = W + K + args.profile_steps

@@ -321,3 +321,62 @@ def linear_backward(dy, x, w, z, act, dz, dx, dw, dbias=None, x_act=ACT_NONE, x_
     _rc(lib.het_linear_backward(_linear_t.pack(rows, inp, out, kind, y_kind, act, x_act, px or 0, ldx, pxq or 0, pxe or 0, pg or 0, pb or 0, pw or 0, ldw, 0, 0, 0, 0, 0,
                                                pz or 0, ldz, pzq or 0, pze or 0, pdy, lddy, pdz or 0, lddz, pdx or 0, lddx, pdw or 0, lddw, pdb or 0, ws or 0, have),
                                 _stream(stream, dev)), "het_linear_backward")
+
+
+class ResidualBlock:
+    """y = x + w2 act(w1 norm(x) + b1) + b2 over rows of `dim` values with `hidden` values inside, in a float32 residual stream: what
+    stands between the rows a lookup hands out (x) and the gradient an update takes (dx).  Weights and what is multiplied are of `dtype`.
+
+    keep8: between the passes the normalised rows and the pre-activations are kept in 8 bits (8.25 bits a value; the layers' inputs are made
+    from them again), else x, mean, rstd, the normalised rows with their weights, z and act(z) are kept whole.  Buffers and the workspace are the
+    block's own and are taken at construction: calls allocate nothing, and a block is used on one stream at a time."""
+
+    def __init__(self, rows, dim, hidden, dtype=None, act=ACT_GELU, eps=1e-5, keep8=True, generator=None, device="cuda"):
+        load()
+        import torch
+        self.rows, self.dim, self.hidden, self.act, self.eps, self.keep8 = rows, dim, hidden, act, eps, keep8
+        dtype = self.dtype = dtype or torch.bfloat16
+
+        def new(*shape, dtype=torch.float32):
+            return torch.empty(*shape, dtype=dtype, device=device)
+
+        self.gamma, self.beta = new(dim).fill_(1), new(dim).zero_()
+        self.w1 = (torch.randn(hidden, dim, generator=generator, device=device) / dim ** 0.5).to(dtype)
+        self.w2 = (torch.randn(dim, hidden, generator=generator, device=device) / hidden ** 0.5).to(dtype)
+        self.b1, self.b2 = new(hidden).zero_(), new(dim).zero_()
+        self.dgamma, self.dbeta, self.dw1, self.dw2 = new(dim), new(dim), new(hidden, dim, dtype=dtype), new(dim, hidden, dtype=dtype)
+        self.db1, self.db2 = new(hidden), new(dim)
+        # between the passes
+        self._h, self._u = new(rows, dim, dtype=dtype), new(rows, hidden, dtype=dtype)
+        self._mean, self._rstd, self._x = new(rows), new(rows), None
+        self._n8 = Packed.empty(rows, dim, device) if keep8 else None
+        self._z = Packed.empty(rows, hidden, device) if keep8 else new(rows, hidden, dtype=dtype)
+        # backward (the forward pass' h and u are free by then if they were kept in 8 bits)
+        self._dz2 = new(rows, dim, dtype=dtype)
+        self._du, self._dh = (self._u, self._h) if keep8 else (new(rows, hidden, dtype=dtype), new(rows, dim, dtype=dtype))
+        need = max(linear_workspace(rows, dim, hidden, dtype), linear_workspace(rows, hidden, dim, dtype), layer_norm_workspace(rows, dim), 16,
+                   linear_workspace(rows, dim, hidden, dtype, True, keep8), linear_workspace(rows, hidden, dim, dtype, True, keep8))
+        self._workspace = new(need, dtype=torch.uint8)
+
+    def parameters(self):
+        """[(parameter, gradient)]; the gradients are written by backward."""
+        return [(self.gamma, self.dgamma), (self.beta, self.dbeta), (self.w1, self.dw1), (self.b1, self.db1), (self.w2, self.dw2), (self.b2, self.db2)]
+
+    def forward(self, x, y):
+        """y of x, both float32 [rows, dim]; x has to stay until backward if activations are kept whole."""
+        layer_norm(x, self.gamma, self.beta, self._h, self._mean, self._rstd, packed=self._n8, eps=self.eps)
+        linear(self._h, self.w1, self.b1, self._u, self.act, z=self._z, workspace=self._workspace)
+        linear(self._u, self.w2, self.b2, y, residual=x, workspace=self._workspace)
+        self._x = None if self.keep8 else x
+
+    def backward(self, dy, dx):
+        """dx and the parameters' gradients from dy (float32 [rows, dim]), once for a forward pass.  dx may be dy itself."""
+        keep8 = self.keep8
+        linear_backward(dy, self._z if keep8 else self._u, self.w2, None, ACT_NONE, self._dz2, self._du, self.dw2, self.db2,
+                        x_act=self.act if keep8 else ACT_NONE, workspace=self._workspace)
+        # dz1 takes du's place: slope and product follow each other
+        linear_backward(self._du, self._n8 if keep8 else self._h, self.w1, self._z, self.act, self._du, self._dh, self.dw1, self.db1,
+                        x_gamma=self.gamma if keep8 else None, x_beta=self.beta if keep8 else None, workspace=self._workspace)
+        layer_norm_backward(self._dh, self._n8 if keep8 else self._x, self.gamma, self._mean, self._rstd, dx, self.dgamma, self.dbeta, residual=dy,
+                            workspace=self._workspace)
+        self._x = None

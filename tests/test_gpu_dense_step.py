@@ -1,0 +1,136 @@
+"""Training with the dense part: lookup, residual block, its backward pass, update, on the GPU against the same in 64 bits on the CPU.
+
+The gradient goes through five products of at most n = 160 terms.  An fp32 sum of n products is off by at most 2 n 2^-24 of the sum of their
+magnitudes, which for terms of either sign is about sqrt(n) times their sum: 5 x 2 x 160 x 2^-24 x sqrt(160) = 1.2e-3 of the gradient.  With
+activations in 8 bits a kept value is off by at most 1/127 of its block's largest, below 5 of the spread, and evenly so: sqrt(1/3) 5 / 127 =
+2.3e-2 of the spread; n enters twice and z once, in squares below 6e-2."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2112_07221_amd import dense
+from paper_2112_07221_amd import hetcache as hc
+
+pytestmark = pytest.mark.gpu
+
+LR = 0.05
+
+
+def gradient64(block, x, target):
+    """dx and the weights' gradients of sum((y - target)^2) / 2, in 64 bits with autograd."""
+    p = [v.detach().cpu().double().requires_grad_() for v in (x, block.gamma, block.beta, block.w1, block.b1, block.w2, block.b2)]
+    x, gamma, beta, w1, b1, w2, b2 = p
+    mean = x.mean(1, keepdim=True)
+    n = (x - mean) / torch.sqrt(((x - mean) ** 2).mean(1, keepdim=True) + 1e-5)
+    z = (n * gamma + beta) @ w1.t() + b1
+    y = x + (z * torch.special.ndtr(z)) @ w2.t() + b2
+    return torch.autograd.grad(((y - target.double()) ** 2).sum() / 2, p)
+
+
+@pytest.mark.parametrize("keep8", [False, True])
+@pytest.mark.parametrize("pooled", [False, True])
+def test_lookup_block_update(pooled, keep8):
+    dev = torch.device("cuda:0")
+    rng = np.random.default_rng(3)
+    vocab, fields, samples, hidden, steps = 700, 8, 37, 160, 5
+    dim = 128 if pooled else 16
+    rows, wide = (samples, dim) if pooled else (samples, fields * dim)
+    table = rng.standard_normal((vocab, dim)).astype(np.float32)
+    want = torch.from_numpy(table).double()
+    W = torch.from_numpy(table.copy()).to(dev)
+    cache = hc.HetCache(300, dim, 0, hc.POLICY_LRU, samples * fields, hc.OPT_SGD, 0.0)
+    cache.attach_backing(W, None, torch.zeros(vocab, dtype=torch.int32, device=dev))
+    g = torch.Generator(device=dev)
+    g.manual_seed(5)
+    block = dense.ResidualBlock(rows, wide, hidden, torch.float32, keep8=keep8, generator=g)
+    block.gamma.add_(0.1 * torch.randn(wide, generator=g, device=dev))
+    block.b1.add_(0.1 * torch.randn(hidden, generator=g, device=dev))
+    out, y, dx = torch.empty(rows, wide, device=dev), torch.empty(rows, wide, device=dev), torch.empty(rows, wide, device=dev)
+    offsets = torch.arange(samples + 1, device=dev) * fields
+    off = 0.0
+    for _ in range(steps):
+        ids_np = (rng.zipf(1.3, samples * fields) % vocab).astype(np.int64)
+        ids, target = torch.from_numpy(ids_np).to(dev), torch.from_numpy(rng.standard_normal((rows, wide)).astype(np.float32))
+        if pooled:
+            cache.lookup_pooled(ids, offsets, out)
+        else:
+            cache.lookup(ids, out)
+        block.forward(out, y)
+        dy = y - target.to(dev)
+        block.backward(dy, dx)
+        if pooled:
+            cache.update_pooled(ids, offsets, dx, LR)
+        else:
+            cache.update(ids, dx, LR)
+        at = torch.from_numpy(ids_np)
+        x64 = want[at].view(samples, fields, dim).sum(1) if pooled else want[at].view(rows, wide)
+        grads = gradient64(block, x64, target)
+        for got, g64 in zip((dx, block.dgamma, block.dbeta, block.dw1, block.db1, block.dw2, block.db2), grads):
+            rel = float((got.cpu().double() - g64).norm() / g64.norm())
+            # (the rows themselves drift from the 64-bit ones by what earlier updates were off: `off` of them)
+            assert rel <= (6e-2 if keep8 else 1.2e-3) + off
+        each = grads[0].repeat_interleave(fields, 0) if pooled else grads[0].view(samples * fields, dim)
+        step = torch.zeros_like(want).index_add_(0, at, each) * LR
+        want -= step
+        off += (6e-2 if keep8 else 1.2e-3) * float(step.norm() / want[at].norm())
+    assert cache.flush() == hc.HET_OK
+    assert cache.stats()["error_bits"] == 0
+    change = want - torch.from_numpy(table).double()
+    rel = float((W.cpu().double() - want).norm() / change.norm())
+    assert rel <= (6e-2 if keep8 else 1.2e-3) * 2          # gradients of five steps, each within its bound; the rows' drift adds less than as much again
+    cache.close()
+
+
+def test_a_captured_block_and_two_blocks_on_two_streams():
+    dev = torch.device("cuda:0")
+    g = torch.Generator(device=dev)
+    g.manual_seed(9)
+    rows, dim = 260, 96
+    blocks = [dense.ResidualBlock(rows, dim, h, t, keep8=k, generator=g) for h, t, k in ((200, torch.bfloat16, True), (320, torch.float16, False))]
+    data = [[torch.randn(rows, dim, generator=g, device=dev) for _ in range(2)] + [torch.empty(rows, dim, device=dev) for _ in range(2)] for _ in blocks]
+
+    def run(b, d):
+        x, dy, y, dx = d
+        b.forward(x, y)
+        b.backward(dy, dx)
+
+    def results(b, d):
+        return [v.clone() for v in [d[2], d[3]] + [g for _, g in b.parameters()]]
+
+    want = []
+    for b, d in zip(blocks, data):
+        run(b, d)
+        want.append(results(b, d))
+    torch.cuda.synchronize()
+    streams, graphs = [torch.cuda.Stream(), torch.cuda.Stream()], []
+    for b, d, s in zip(blocks, data, streams):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            run(b, d)
+        graphs.append(graph)
+    for _ in range(4):
+        for b, d in zip(blocks, data):
+            d[2].fill_(7)
+            d[3].fill_(7)
+        torch.cuda.synchronize()
+        for graph, s in zip(graphs, streams):                  # both at once: each has its own workspace
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        for b, d, w in zip(blocks, data, want):
+            for got, x in zip(results(b, d), w):
+                assert torch.equal(got, x)
+
+
+def test_the_gradient_may_take_the_place_of_the_outputs():
+    g = torch.Generator(device="cuda")
+    g.manual_seed(2)
+    b = dense.ResidualBlock(50, 40, 64, torch.bfloat16, generator=g)
+    x, dy, y, dx = [torch.randn(50, 40, generator=g, device="cuda") for _ in range(4)]
+    b.forward(x, y)
+    b.backward(dy, dx)
+    b.forward(x, y)
+    b.backward(dy, dy)
+    assert torch.equal(dx, dy)
