@@ -68,14 +68,16 @@ constexpr int64_t CUS = 256;
 
 // Microseconds a product takes with tiles of 256 or 128 and its k's split, by the times measured at 64 .. 8192 rows, columns and k's in bf16 and
 // fp32: a tile of 256 has a compute unit to itself, of 128 two share one.  Adding up the splits costs a launch and the sums' way through memory.
+// 4096 x 1664 -> 4096 in bf16: 256 48, 128 54 us; 2048 x 2048 -> 2048: 43 and 27; dw of 16384 x 896 -> 4096: 128 175, split in two 126, 256 split in
+// four 129.  Tiles of 256 x 128 (two waves' 64 x 64 side by side, one workgroup a compute unit) were slower than one of the two everywhere.
 static double tiles_us(int tile, int64_t tiles, int64_t splits, int64_t steps, int64_t m, int64_t n, bool f32, bool aligned)
 {
     const double s = (double)((steps + splits - 1) / splits) * (aligned ? 1.0 : f32 ? 1.2 : 2.0);
     const int64_t groups = tiles * splits, turns = (groups + CUS - 1) / CUS;
     double us = 0;
     if (tile == 256) us = (double)turns * (10 + (f32 ? 7.3 : 1.5) * s);
-    else us = (double)(turns / 2) * (6 + (f32 ? 4.1 : 0.86) * s) + (double)(turns % 2) * (4 + (f32 ? 2.1 : 0.5) * s);
-    return splits > 1 ? us + 4 + (double)splits * (double)m * (double)n * 2e-6 : us;
+    else us = (double)(turns / 2) * (6 + (f32 ? 4.1 : 0.8) * s) + (double)(turns % 2) * (4 + (f32 ? 2.1 : 0.62) * s);
+    return splits > 1 ? us + 3 + (double)splits * (double)m * (double)n * 1.4e-6 : us;
 }
 
 // ... and with product_small_kernel: its waves' turns through k (a step is a span, two of them at a time), a thousand workgroups at a time, and the
