@@ -133,7 +133,11 @@ int het_linear(const het_linear_t *l, void *hip_stream);
  */
 int het_linear_backward(const het_linear_t *l, void *hip_stream);
 
-/* Bytes of workspace, from rows, in, out, type, xq, dx, dw and dbias of `l` (the pointers: NULL or not); negative: HET_EINVAL. */
+/*
+ * Bytes of workspace of a call with these fields: rows, in, out, type, x, ldx, w, ldw and (backward) dy, lddy, dz, lddz, xq, dx, dw, dbias.  Of the pointers it
+ * matters whether they are NULL and whether they are aligned to 16: operands whose rows do not begin at multiples of 16 bytes, or are
+ * not a multiple of 16 bytes wide, may be laid out in the workspace.  Negative: HET_EINVAL.
+ */
 int64_t het_linear_workspace(const het_linear_t *l, int32_t backward);
 
 #ifdef __cplusplus

@@ -65,6 +65,19 @@ void with_type(int32_t t, F &&f)
     else if (t == HET_BF16) f(Tag<bf16>());
     else f(Tag<f16>());
 }
+void launch_expand(const ExpandArgs &a, int32_t type, hipStream_t st)
+{
+    const uint32_t blocks = (uint32_t)cdiv(a.rows * cdiv(a.dim, CHUNK), 256);
+    with_type(type, [&](auto t) { expand_kernel<typename decltype(t)::type><<<blocks, 256, 0, st>>>(a); });
+}
+
+// An operand laid out at `to`, which it then is.
+void lay(const void *&p, int64_t &ld, int64_t rows, int32_t width, void *to, int32_t type, hipStream_t st)
+{
+    if (rows > 0) launch_lay(p, ld, rows, width, to, type, st);
+    p = to; ld = laid_pitch(width, type);
+}
+
 bool known_pair(int32_t x, int32_t y) { return known_type(x) && known_type(y) && (x == y || x == HET_F32); }
 
 bool pack_sizes(int64_t rows, int32_t dim) { return rows >= 0 && rows <= MOST_ROWS && dim >= 1 && dim <= MOST_DIM && rows * dim <= MOST_VALUES; }
@@ -90,48 +103,58 @@ int slope_splits(int64_t rows, int32_t out)
     return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)PARTIALS, cdiv(rows, 8 * SLOPE_ROWS), cdiv(2048, cdiv(out, SLOPE_COLS))}));
 }
 
-struct BackPlan {
-    ProductPlan dx, dw;
-    int slope;                  // workgroups down the rows
-    int64_t bias_at, x_at, partial_at, bytes;
-    const void *dz, *x;         // the products' operands
-    int64_t lddz, ldx;
+// Where a call's scratch lies in its workspace, from 0 on in order, each piece at a multiple of 16 bytes.
+struct Room {
+    int64_t bytes = 0;
+    int64_t take(int64_t n) { const int64_t at = bytes; bytes += align16(n); return at; }
+    int64_t take_laid(bool lay, int64_t rows, int64_t width, int32_t type) { return take(lay ? rows * laid_pitch(width, type) * size_of(type) : 0); }
 };
 
-// sizes_only: the workspace's size is asked for, and nobody knows yet how the operands lie: the larger of what the kernels for either take.
-ProductPlan plan_of(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k, const void *a, int64_t lda, const void *b, int64_t ldb, bool sizes_only)
+struct ForwardPlan {
+    ProductPlan y;
+    int64_t partial_at, x_at, w_at, bytes;
+};
+
+ForwardPlan forward_plan(const het_linear_t *l)
 {
-    if (!sizes_only)
-        return product_plan(m, n, k, type, a_k, b_k, product_copies(a, lda, (int)(a_k ? k : m), type) && product_copies(b, ldb, (int)(b_k ? k : n), type));
-    ProductPlan p = product_plan(m, n, k, type, a_k, b_k, true);
-    p.partial_bytes = std::max(p.partial_bytes, product_plan(m, n, k, type, a_k, b_k, false).partial_bytes);
+    ForwardPlan p;
+    Room room;
+    p.y = product_plan(l->rows, l->out, l->in, l->type, true, true, product_lies(l->x, l->ldx, l->in, l->type), product_lies(l->w, l->ldw, l->in, l->type));
+    p.partial_at = room.take(p.y.partial_bytes);
+    p.x_at = room.take_laid(p.y.lay_a, l->rows, l->in, l->type);
+    p.w_at = room.take_laid(p.y.lay_b, l->out, l->in, l->type);
+    p.bytes = room.bytes;
     return p;
 }
 
-BackPlan back_plan(const het_linear_t *l, bool sizes_only)
+struct BackPlan {
+    ProductPlan dx{}, dw{};
+    int slope;                  // workgroups down the rows
+    bool runs_slope, lay_dz;
+    int64_t bias_at, partial_at, dz_at, w_at, x_at, ldx, bytes;
+};
+
+BackPlan back_plan(const het_linear_t *l)
 {
     BackPlan p;
+    Room room;
+    const void *dz = l->dz ? l->dz : l->dy;
+    const bool dz_lies = product_lies(dz, l->dz ? l->lddz : l->lddy, l->out, l->type);
+    p.runs_slope = l->dz || l->dbias;
     p.slope = slope_splits(l->rows, l->out);
-    p.bias_at = 0;
-    p.x_at = l->dbias ? align16((int64_t)p.slope * width_of(l->out) * 4) : 0;
-    p.partial_at = p.x_at + (l->xq && l->dw ? align16(l->rows * (int64_t)l->in * size_of(l->type)) : 0);
-    p.dz = l->dz ? l->dz : l->dy;
-    p.lddz = l->dz ? l->lddz : l->lddy;
-    p.x = l->xq ? static_cast<const char *>(l->workspace) + p.x_at : static_cast<const char *>(l->x);
-    p.ldx = l->xq ? l->in : l->ldx;
-    p.bytes = p.partial_at;
-    if (l->dx) {
-        p.dx = plan_of(l->rows, l->in, l->out, l->type, true, false, p.dz, p.lddz, l->w, l->ldw, sizes_only);
-        p.bytes = p.partial_at + p.dx.partial_bytes;
-    }
-    if (l->dw) {
-        p.dw = plan_of(l->out, l->in, l->rows, l->type, false, false, p.dz, p.lddz, p.x, p.ldx, sizes_only);
-        p.bytes = std::max(p.bytes, p.partial_at + p.dw.partial_bytes);
-    }
+    if (l->dx) p.dx = product_plan(l->rows, l->in, l->out, l->type, true, false, dz_lies, product_lies(l->w, l->ldw, l->in, l->type));
+    // x in 8 bits is expanded into rows that lie well
+    p.ldx = l->xq ? laid_pitch(l->in, l->type) : l->ldx;
+    if (l->dw) p.dw = product_plan(l->out, l->in, l->rows, l->type, false, false, dz_lies, l->xq || product_lies(l->x, l->ldx, l->in, l->type));
+    p.lay_dz = p.dx.lay_a || p.dw.lay_a;
+    p.bias_at = room.take(l->dbias ? (int64_t)p.slope * width_of(l->out) * 4 : 0);
+    p.partial_at = room.take(std::max(p.dx.partial_bytes, p.dw.partial_bytes));
+    p.dz_at = room.take_laid(p.lay_dz, l->rows, l->out, l->type);
+    p.w_at = room.take_laid(p.dx.lay_b, l->out, l->in, l->type);
+    p.x_at = room.take_laid(l->dw && (l->xq || p.dw.lay_b), l->rows, l->in, l->type);
+    p.bytes = room.bytes;
     return p;
 }
-
-ProductPlan forward_plan(const het_linear_t *l, bool sizes_only) { return plan_of(l->rows, l->out, l->in, l->type, true, true, l->x, l->ldx, l->w, l->ldw, sizes_only); }
 
 bool workspace_ok(const void *ws, int64_t have, int64_t need) { return need == 0 || (ws && aligned16(ws) && have >= need); }
 
@@ -199,17 +222,15 @@ int het_expand(const int8_t *q, const uint8_t *e, int64_t rows, int32_t dim, con
 {
     if (!pack_sizes(rows, dim) || !known_type(type) || !known_act(act) || ldy < dim) return HET_EINVAL;
     if (rows == 0) return HET_OK;
-    const int64_t blocks = cdiv(rows * cdiv(dim, CHUNK), 256);
     if (!y || !q || !e || !aligned16(q)) return HET_EINVAL;
-    ExpandArgs a{q, e, gamma, beta, y, ldy, rows, dim, pitch_of(dim), act};
-    with_type(type, [&](auto t) { expand_kernel<typename decltype(t)::type><<<(uint32_t)blocks, 256, 0, static_cast<hipStream_t>(hip_stream)>>>(a); });
+    launch_expand(ExpandArgs{q, e, gamma, beta, y, ldy, rows, dim, pitch_of(dim), act}, type, static_cast<hipStream_t>(hip_stream));
     return launched();
 }
 
 int64_t het_linear_workspace(const het_linear_t *l, int32_t backward)
 {
     if (!linear_sizes(l)) return HET_EINVAL;
-    return backward ? back_plan(l, true).bytes : forward_plan(l, true).partial_bytes;
+    return backward ? back_plan(l).bytes : forward_plan(l).bytes;
 }
 
 int het_linear(const het_linear_t *l, void *hip_stream)
@@ -218,11 +239,15 @@ int het_linear(const het_linear_t *l, void *hip_stream)
     if (l->ldx < l->in || l->ldw < l->in || l->ldy < l->out || (l->residual && l->ld_residual < l->out) || (l->z && l->ldz < l->out) || !l->zq != !l->ze) return HET_EINVAL;
     if (l->rows == 0) return HET_OK;
     if (!l->x || !l->w || !l->y || !aligned16(l->zq)) return HET_EINVAL;
-    const ProductPlan p = forward_plan(l, false);
-    if (!p.ok || !workspace_ok(l->workspace, l->workspace_bytes, p.partial_bytes)) return HET_EINVAL;
+    const ForwardPlan p = forward_plan(l);
+    if (!p.y.ok || !workspace_ok(l->workspace, l->workspace_bytes, p.bytes)) return HET_EINVAL;
+    const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    char *ws = static_cast<char *>(l->workspace);
     ProductArgs a{};
     a.a = l->x; a.lda = l->ldx; a.b = l->w; a.ldb = l->ldw;
-    a.partial = static_cast<float *>(l->workspace);
+    if (p.y.lay_a) lay(a.a, a.lda, l->rows, l->in, ws + p.x_at, l->type, st);
+    if (p.y.lay_b) lay(a.b, a.ldb, l->out, l->in, ws + p.w_at, l->type, st);
+    a.partial = reinterpret_cast<float *>(ws + p.partial_at);
     a.f.bias = l->bias;
     a.f.residual = l->residual; a.f.ldr = l->ld_residual;
     a.f.y = l->y; a.f.ldy = l->ldy;
@@ -230,7 +255,7 @@ int het_linear(const het_linear_t *l, void *hip_stream)
     a.f.q = l->zq; a.f.e = l->ze; a.f.pitch = pitch_of(l->out);
     a.f.act = l->act;
     a.f.y_f32 = l->y_type == HET_F32;
-    launch_product(a, p, l->type, true, true, static_cast<hipStream_t>(hip_stream));
+    launch_product(a, p.y, l->type, true, true, st);
     return launched();
 }
 
@@ -248,38 +273,47 @@ int het_linear_backward(const het_linear_t *l, void *hip_stream)
         if (!l->dy || (has_act && !l->zq && !l->z) || (has_act && !aligned16(l->zq))) return HET_EINVAL;
         if ((l->dx && !l->w) || (l->dw && !l->xq && !l->x) || (l->dw && !aligned16(l->xq))) return HET_EINVAL;
     }
-    const BackPlan p = back_plan(l, false);
+    const BackPlan p = back_plan(l);
     if ((l->dx && !p.dx.ok) || (l->dw && !p.dw.ok) || !workspace_ok(l->workspace, l->workspace_bytes, p.bytes)) return HET_EINVAL;
     if (!some && !l->dw && !l->dbias) return HET_OK;
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     char *ws = static_cast<char *>(l->workspace);
-    if (l->dz || l->dbias) {
+    const void *dz = dz_is_dy ? l->dy : l->dz, *laid = dz;
+    int64_t lddz = dz_is_dy ? l->lddy : l->lddz, ld_laid = lddz;
+    if (p.runs_slope) {
         SlopeArgs s{};
         s.dy = l->dy; s.lddy = l->lddy;
         s.z = l->z; s.ldz = l->ldz; s.q = l->zq; s.e = l->ze;
         s.dz = l->dz; s.lddz = l->lddz;
+        if (p.lay_dz) { laid = s.laid = ws + p.dz_at; ld_laid = s.laid_pitch = laid_pitch(l->out, l->type); }
         s.partial = l->dbias ? reinterpret_cast<float *>(ws + p.bias_at) : nullptr;
         s.rows = l->rows; s.dim = l->out; s.pitch = pitch_of(l->out); s.act = l->act;
         const dim3 grid((uint32_t)cdiv(l->out, SLOPE_COLS), (uint32_t)p.slope);
         with_types(l->y_type, l->type, [&](auto ty, auto t) { launch_slope<typename decltype(t)::type, typename decltype(ty)::type>(s, grid, st); });
         if (l->dbias) launch_column_sum(s.partial, p.slope, 1, l->out, l->dbias, nullptr, st);
+    } else if (p.lay_dz) {
+        lay(laid, ld_laid, l->rows, l->out, ws + p.dz_at, l->type, st);
     }
+    ProductArgs a{};
+    a.partial = reinterpret_cast<float *>(ws + p.partial_at);
+    a.f.y_f32 = l->type == HET_F32;
     if (l->dx && some) {
-        ProductArgs a{};
-        a.a = p.dz; a.lda = p.lddz; a.b = l->w; a.ldb = l->ldw;
-        a.partial = reinterpret_cast<float *>(ws + p.partial_at);
-        a.f.y = l->dx; a.f.ldy = l->lddx; a.f.y_f32 = l->type == HET_F32;
+        a.a = p.dx.lay_a ? laid : dz; a.lda = p.dx.lay_a ? ld_laid : lddz;
+        a.b = l->w; a.ldb = l->ldw;
+        if (p.dx.lay_b) lay(a.b, a.ldb, l->out, l->in, ws + p.w_at, l->type, st);
+        a.f.y = l->dx; a.f.ldy = l->lddx;
         launch_product(a, p.dx, l->type, true, false, st);
     }
     if (l->dw) {
-        if (l->xq && some) {
-            const int rc = het_expand(l->xq, l->xe, l->rows, l->in, l->x_gamma, l->x_beta, l->x_act, ws + p.x_at, l->type, l->in, hip_stream);
-            if (rc != HET_OK) return rc;
+        a.a = p.dw.lay_a ? laid : dz; a.lda = p.dw.lay_a ? ld_laid : lddz;
+        a.b = l->x; a.ldb = l->ldx;
+        if (l->xq) {
+            a.b = ws + p.x_at; a.ldb = p.ldx;
+            if (some) launch_expand(ExpandArgs{l->xq, l->xe, l->x_gamma, l->x_beta, ws + p.x_at, p.ldx, l->rows, l->in, pitch_of(l->in), l->x_act}, l->type, st);
+        } else if (p.dw.lay_b) {
+            lay(a.b, a.ldb, l->rows, l->in, ws + p.x_at, l->type, st);
         }
-        ProductArgs a{};
-        a.a = p.dz; a.lda = p.lddz; a.b = p.x; a.ldb = p.ldx;
-        a.partial = reinterpret_cast<float *>(ws + p.partial_at);
-        a.f.y = l->dw; a.f.ldy = l->lddw; a.f.y_f32 = l->type == HET_F32;
+        a.f.y = l->dw; a.f.ldy = l->lddw;
         launch_product(a, p.dw, l->type, false, false, st);
     }
     return launched();

@@ -41,17 +41,15 @@ void launch_product_of(const ProductArgs &a, const ProductPlan &p, bool a_k, boo
         return;
     }
     const uint32_t grid = (uint32_t)(a.tiles_m * a.tiles_n * a.splits);
-    if (p.aligned && p.tile == 256) {
+    if (p.tile == 256) {
         if (a_k && b_k) product_kernel<T, true, true, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
         else if (a_k) product_kernel<T, true, false, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
         else product_kernel<T, false, false, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
-    } else if (p.aligned) {
+    } else {
         if (a_k && b_k) product_kernel<T, true, true, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
         else if (a_k) product_kernel<T, true, false, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
         else product_kernel<T, false, false, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
-    } else if (a_k && b_k) product_any_kernel<T, true, true><<<grid, 256, 0, st>>>(a);
-    else if (a_k) product_any_kernel<T, true, false><<<grid, 256, 0, st>>>(a);
-    else product_any_kernel<T, false, false><<<grid, 256, 0, st>>>(a);
+    }
     if (a.splits > 1) {
         const int64_t per = (a.n + PACK_BLOCK - 1) / PACK_BLOCK * 4;
         join_kernel<T><<<(uint32_t)((a.m * per + 255) / 256), 256, 0, st>>>(a);
@@ -70,9 +68,9 @@ constexpr int64_t CUS = 256;
 // fp32: a tile of 256 has a compute unit to itself, of 128 two share one.  Adding up the splits costs a launch and the sums' way through memory.
 // 4096 x 1664 -> 4096 in bf16: 256 48, 128 54 us; 2048 x 2048 -> 2048: 43 and 27; dw of 16384 x 896 -> 4096: 128 175, split in two 126, 256 split in
 // four 129.  Tiles of 256 x 128 (two waves' 64 x 64 side by side, one workgroup a compute unit) were slower than one of the two everywhere.
-static double tiles_us(int tile, int64_t tiles, int64_t splits, int64_t steps, int64_t m, int64_t n, bool f32, bool aligned)
+static double tiles_us(int tile, int64_t tiles, int64_t splits, int64_t steps, int64_t m, int64_t n, bool f32)
 {
-    const double s = (double)((steps + splits - 1) / splits) * (aligned ? 1.0 : f32 ? 1.2 : 2.0);
+    const double s = (double)((steps + splits - 1) / splits);
     const int64_t groups = tiles * splits, turns = (groups + CUS - 1) / CUS;
     double us = 0;
     if (tile == 256) us = (double)turns * (10 + (f32 ? 7.3 : 1.5) * s);
@@ -91,26 +89,31 @@ static double small_us(int64_t steps, int64_t m, int64_t n, int64_t k, bool a_k,
            each * (double)high * (double)wide * (double)k;
 }
 
-ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k, bool aligned)
+// ... and laying out an operand: a launch, and its way there and back through memory.
+static double lay_us(int64_t rows, int64_t width, bool f32) { return 3 + (double)rows * (double)width * (f32 ? 8 : 4) / 4e6; }
+
+ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k, bool lies_a, bool lies_b)
 {
+    const bool f32 = type == HET_F32;
     ProductPlan p{};
-    p.aligned = aligned;
+    p.lay_a = !lies_a; p.lay_b = !lies_b;
     p.m = (int)m; p.n = (int)n; p.k = (int)k;
-    p.splits = 1; p.k_split = (int)k; p.tile = ANY_TILE;
-    p.ok = true;
-    const int64_t step = type == HET_F32 ? 32 : 64, steps = (k + step - 1) / step;
+    p.splits = 1;
+    const int64_t step = f32 ? 32 : 64, steps = (k + step - 1) / step;
     double best = 1e30;
-    for (int tile = aligned ? 256 : ANY_TILE; tile >= 128; tile /= 2) {
+    for (int tile = 256; tile >= 128; tile /= 2) {
         const int64_t tiles = ((m + tile - 1) / tile) * ((n + tile - 1) / tile);
         for (int64_t splits = 1; splits <= 32 && (splits == 1 || (splits * 4 <= steps && tiles * splits <= 2 * CUS)); ++splits) {
-            const double us = tiles_us(tile, tiles, splits, steps, m, n, type == HET_F32, aligned);
+            const double us = tiles_us(tile, tiles, splits, steps, m, n, f32);
             if (us < best) { best = us; p.tile = tile; p.splits = (int)splits; }
         }
     }
-    if (small_us(steps, m, n, k, a_k, b_k, type == HET_F32) < best) {
+    best += (p.lay_a ? lay_us(m, k, f32) : 0) + (p.lay_b ? lay_us(n, k, f32) : 0);
+    if (small_us(steps, m, n, k, a_k, b_k, f32) < best) {
         p.small_m = a_k && b_k && m <= 16 ? 1 : 2;
         p.small_n = ((m + 31) / 32) * ((n + 31) / 32) < CUS ? 1 : 2;
         p.splits = 1;
+        p.lay_a = p.lay_b = false;
     }
     p.k_split = (int)((steps + p.splits - 1) / p.splits * step);
     p.splits = (int)std::max<int64_t>(1, (k + p.k_split - 1) / std::max(p.k_split, 1));
@@ -119,11 +122,21 @@ ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bo
     return p;
 }
 
-// Whether product_kernel takes an operand as it lies: rows at multiples of 16 bytes, whole pieces of them along k or across, and a tile within 2 GB.
-bool product_copies(const void *p, int64_t ld, int width, int type)
+// Whether product_kernel takes an operand as it lies: rows at multiples of 16 bytes and of whole pieces, a tile within 2 GB.
+bool product_lies(const void *p, int64_t ld, int64_t width, int type)
 {
     const int64_t size = type == HET_F32 ? 4 : 2;
     return (reinterpret_cast<uintptr_t>(p) & 15) == 0 && ld * size % 16 == 0 && width * size % 16 == 0 && 256 * ld * size < (1ll << 31);
+}
+
+int64_t laid_pitch(int64_t width, int type) { return type == HET_F32 ? (width + 3) / 4 * 4 : (width + 7) / 8 * 8; }
+
+void launch_lay(const void *p, int64_t ld, int64_t rows, int width, void *to, int type, hipStream_t st)
+{
+    const int64_t pitch = laid_pitch(width, type), pieces = rows * (pitch / (type == HET_F32 ? 4 : 8));
+    const uint32_t grid = (uint32_t)((pieces + 255) / 256);
+    if (type == HET_F32) lay_kernel<uint32_t><<<grid, 256, 0, st>>>(static_cast<const uint32_t *>(p), ld, rows, width, static_cast<uint32_t *>(to), (int)pitch);
+    else lay_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(p), ld, rows, width, static_cast<uint16_t *>(to), (int)pitch);
 }
 
 void launch_product(ProductArgs a, const ProductPlan &p, int type, bool a_k, bool b_k, hipStream_t st)

@@ -114,29 +114,6 @@ struct Tile {
         if (sizeof(T) == 2) return r * WIDE + (c ^ (4 * (r & 3)));
         return r * WIDE + (c ^ (8 * ((r >> 2) & 1)));
     }
-    // Piece `i` of the tile (0 .. PIECES - 1) from memory: rows [row0, rows), k's [k0, k_end).  k's outside are zero; rows outside are the last row's
-    // copies (what comes of them is not stored).  A piece that would cross the end of a row in memory is the row's last 16 bytes, shifted: no lane takes a
-    // branch of its own, and the loads of all pieces are under way together.
-    __device__ static __forceinline__ i32x4 load(const T *p, int64_t ld, int i, int row0, int rows, int k0, int k_end)
-    {
-        const int along = i % WIDE, down = i / WIDE;
-        const int outer = (K ? row0 : k0) + down, inner = (K ? k0 : row0) + along * PIECE, most = K ? rows : k_end, end = K ? k_end : rows;
-        const T *row = p + (int64_t)(outer < most ? outer : most - 1) * ld;
-        if (end < PIECE) {                                        // the whole row is less than a piece
-            vec<T, PIECE> v = {};
-#pragma unroll
-            for (int j = 0; j < PIECE - 1; ++j) if (inner + j < end && outer < most) v[j] = row[inner + j];
-            return __builtin_bit_cast(i32x4, v);
-        }
-        const int from = inner < end - PIECE ? inner : end - PIECE, over = inner - from;
-        unsigned __int128 v;
-        __builtin_memcpy(&v, row + from, 16);
-        if (end % PIECE) v >>= over < PIECE ? 8 * (int)sizeof(T) * over : 0;
-        if (over >= PIECE || (!K && outer >= most)) v = 0;
-        return __builtin_bit_cast(i32x4, v);
-    }
-    __device__ static __forceinline__ int place(int i) { return mixed(i / WIDE, i % WIDE); }
-
     // Frag `s` (0 .. 3) of the 32 rows from r0.
     __device__ static __forceinline__ F read(const i32x4 *lds, int r0, int s)
     {
@@ -272,7 +249,8 @@ __device__ __forceinline__ f32x4 *finish_room(i32x4 *first, i32x4 *second)
 // ---- aligned operands -------------------------------------------------------------------------------------
 // TM x TN tiles, WM x WN waves.  Memory goes straight to LDS, 16 bytes a lane, one step ahead of the products: the next step's pieces are on their way
 // while a step is multiplied, and nothing passes through registers.  Pieces behind an edge are asked for outside the buffer's range, which
-// reads as zero.  Operands' rows begin at multiples of 16 bytes and their widths are whole pieces (the host looks).
+// reads as zero.  Operands' rows begin at multiples of 16 bytes and are whole pieces wide; others are laid out so first (lay_kernel): pieces taken
+// through registers from rows that begin anywhere cost more (2051 x 3001 -> 2049 in bf16 172 us, laid out 51; in fp32 484 and 275).
 __device__ __forceinline__ void copies_done() { __builtin_amdgcn_s_waitcnt(0x0F70); }        // vmcnt(0) alone
 
 template <typename T, int R, bool K, bool PERMUTED, int THREADS>
@@ -391,56 +369,24 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
     }
 }
 
-// ---- any size, any stride ---------------------------------------------------------------------------------
-// 128 x 128 tiles, four waves of 64 x 64.  Pieces go through registers, where edges are cut off: the next step's are under way while this one's are multiplied.
-constexpr int ANY_TILE = 128;
-
-template <typename T, bool AK, bool BK>
-__global__ __launch_bounds__(256) void product_any_kernel(ProductArgs a)
+// Rows that begin anywhere -> rows of `pitch` values that begin at multiples of 16 bytes, zero behind the end.  A piece a thread.
+template <typename U>
+__global__ __launch_bounds__(256) void lay_kernel(const U *p, int64_t ld, int64_t rows, int width, U *to, int pitch)
 {
-    using TA = Tile<T, ANY_TILE, AK, false>;
-    using TB = Tile<T, ANY_TILE, BK, true>;
-    __shared__ i32x4 la[TA::PIECES], lb[TB::PIECES];
-    const int tiles = a.tiles_m * a.tiles_n, split = blockIdx.x / tiles;
-    int tm, tn;
-    tile_at(tile_of(blockIdx.x % tiles, tiles), a.tiles_m, a.tiles_n, tm, tn);
-    const int row0 = tm * ANY_TILE, col0 = tn * ANY_TILE;
-    const int k_begin = split * a.k_split, k_end = a.k - k_begin < a.k_split ? a.k : k_begin + a.k_split;
-    const T *pa = static_cast<const T *>(a.a), *pb = static_cast<const T *>(a.b);
-    const int wave = threadIdx.x / 64, wm = (wave / 2) * 64, wn = (wave % 2) * 64;
-
-    i32x4 ra[4], rb[4];
-    auto fetch = [&](int k0) {
+    constexpr int PIECE = 16 / (int)sizeof(U);
+    const int per = pitch / PIECE;
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+    if (row >= rows) return;
+    const int at = (int)(i - row * per) * PIECE;
+    const U *from = p + row * ld;
+    vec<U, PIECE> v = {};
+    if (at + PIECE <= width) {
+        __builtin_memcpy(&v, from + at, 16);
+    } else {
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            ra[u] = TA::load(pa, a.lda, threadIdx.x + u * 256, row0, a.m, k0, k_end);
-            rb[u] = TB::load(pb, a.ldb, threadIdx.x + u * 256, col0, a.n, k0, k_end);
-        }
-    };
-    f32x16 acc[2][2] = {};
-    if (k_begin < k_end) fetch(k_begin);
-    for (int k0 = k_begin; k0 < k_end; k0 += TA::STEP) {
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < 4; ++u) { la[TA::place(threadIdx.x + u * 256)] = ra[u]; lb[TB::place(threadIdx.x + u * 256)] = rb[u]; }
-        __syncthreads();
-        if (k0 + TA::STEP < k_end) fetch(k0 + TA::STEP);
-#pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            typename TA::F fa[2];
-            typename TB::F fb[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) { fa[i] = TA::read(la, wm + 32 * i, s); fb[i] = TB::read(lb, wn + 32 * i, s); }
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[i][j] = multiply(fb[j], fa[i], acc[i][j]);
-        }
+        for (int j = 0; j < PIECE - 1; ++j) if (at + j < width) v[j] = from[at + j];
     }
-    __syncthreads();
-    f32x4 *room = finish_room<4>(la, lb);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) finish_tile<T>(a, split, row0 + wm + 32 * i, col0 + wn, acc[i][0], acc[i][1], room);
+    *reinterpret_cast<vec<U, PIECE> *>(to + row * pitch + at) = v;
 }
 
 // Adds the splits' sums in their order and ends them.  A chunk a thread, four for each block of 32 columns (the 8-bit copy needs them side by side).

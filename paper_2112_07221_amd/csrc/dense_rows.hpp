@@ -313,8 +313,9 @@ struct SlopeArgs {
     const int8_t *q;         // z in 8 bits; null: z, or no activation
     const uint8_t *e;
     void *dz;
+    void *laid;              // dz once more, as product_kernel takes it, or null
     float *partial;          // null: no bias
-    int64_t lddy, ldz, lddz, rows;
+    int64_t lddy, ldz, lddz, laid_pitch, rows;
     int dim, pitch, act;
 };
 
@@ -356,6 +357,12 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
                     for (int j = 0; j < 8; ++j) d[j] *= slope[j];
                 }
                 if (a.dz) store_row<WHOLE>(static_cast<T *>(a.dz) + at * a.lddz, c, a.dim, d);
+                if (a.laid) {
+                    f32x8 whole = d;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) whole[j] = (WHOLE || j < n) ? d[j] : 0.f;
+                    store_row<WHOLE>(static_cast<T *>(a.laid) + at * a.laid_pitch, c, (int)a.laid_pitch, whole);
+                }
 #pragma unroll
                 for (int j = 0; j < 8; ++j) s[j] += (WHOLE || j < n) ? d[j] : 0.f;
             }

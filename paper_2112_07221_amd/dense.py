@@ -243,15 +243,20 @@ def expand(packed, y, act=ACT_NONE, gamma=None, beta=None, stream=None):
 
 
 @functools.lru_cache(maxsize=4096)
-def _linear_workspace(rows, inp, out, kind, backward, xq, dx, dw, dbias):
-    l = linear_struct(rows=rows, inp=inp, out=out, type=kind, xq=xq, dx=dx, dw=dw, dbias=dbias)
+def _linear_workspace(rows, inp, out, kind, backward, x, ldx, w, ldw, dz, lddz, xq, dx, dw, dbias):
+    """Of the operands' addresses only what they are modulo 16 matters: callers pass 16 + that."""
+    l = linear_struct(rows=rows, inp=inp, out=out, type=kind, x=x, ldx=ldx, w=w, ldw=ldw, dz=dz, lddz=lddz, xq=xq, dx=dx, dw=dw, dbias=dbias)
     return (_lib or load()).het_linear_workspace(l, backward)
 
 
-def linear_workspace(rows, inp, out, dtype, backward=False, x_packed=False, dx=True, dw=True, dbias=True):
-    """Bytes of workspace linear or linear_backward takes; x_packed: x is kept in 8 bits; dx, dw, dbias: which of them are wanted."""
+def linear_workspace(rows, inp, out, dtype, backward=False, x_packed=False, dx=True, dw=True, dbias=True, views=False):
+    """Bytes of workspace linear or linear_backward takes.  x_packed: x is kept in 8 bits; dx, dw, dbias: which of them are wanted; views: x, w
+    and dz may lie in wider matrices or begin anywhere (else they are contiguous and begin at multiples of 16 bytes)."""
     load()
-    return _linear_workspace(rows, inp, out, _types[dtype], int(backward), int(x_packed), int(dx), int(dw), int(dbias))
+    kind = _types[dtype]
+    at = (16, 17) if views else (16,)
+    return max(_linear_workspace(rows, inp, out, kind, int(backward), x, inp, w, inp, dz, out, int(x_packed), int(dx), int(dw), int(dbias))
+               for x in at for w in at for dz in at)
 
 
 def linear(x, w, bias, y, act=ACT_NONE, residual=None, z=None, workspace=None, stream=None):
@@ -272,7 +277,7 @@ def linear(x, w, bias, y, act=ACT_NONE, residual=None, z=None, workspace=None, s
         zq, ze = _packed(z, "z", rows, out, dev)
     elif z is not None:
         pz, ldz, _ = _matrix(z, "z", rows, out, dev, x.dtype)
-    keep, ws, have = _scratch(_linear_workspace(rows, inp, out, kind, 0, 0, 0, 0, 0), workspace, stream, dev)
+    keep, ws, have = _scratch(_linear_workspace(rows, inp, out, kind, 0, px % 16 + 16, ldx, pw % 16 + 16, ldw, 0, 0, 0, 0, 0, 0), workspace, stream, dev)
     _rc(lib.het_linear(_linear_t.pack(rows, inp, out, kind, y_kind, act, 0, px, ldx, 0, 0, 0, 0, pw, ldw, _vector(bias, "bias", out, dev) or 0, pr or 0, ldr, py, ldy,
                                       pz or 0, ldz, zq or 0, ze or 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, ws or 0, have), _stream(stream, dev)), "het_linear")
 
@@ -316,7 +321,8 @@ def linear_backward(dy, x, w, z, act, dz, dx, dw, dbias=None, x_act=ACT_NONE, x_
             if x_act != ACT_NONE or x_gamma is not None or x_beta is not None:
                 raise ValueError("x_act, x_gamma and x_beta are for an x kept in 8 bits")
     pdb = _vector(dbias, "dbias", out, dev)
-    need = _linear_workspace(rows, inp, out, kind, 1, int(bool(pxq)), int(bool(pdx)), int(bool(pdw)), int(bool(pdb)))
+    need = _linear_workspace(rows, inp, out, kind, 1, (px or 0) % 16 + 16, ldx, (pw or 0) % 16 + 16, ldw, (pdz or pdy) % 16 + 16, lddz if pdz else lddy, 1 if pxq else 0,
+                             1 if pdx else 0, 1 if pdw else 0, 1 if pdb else 0)
     keep, ws, have = _scratch(need, workspace, stream, dev)
     _rc(lib.het_linear_backward(_linear_t.pack(rows, inp, out, kind, y_kind, act, x_act, px or 0, ldx, pxq or 0, pxe or 0, pg or 0, pb or 0, pw or 0, ldw, 0, 0, 0, 0, 0,
                                                pz or 0, ldz, pzq or 0, pze or 0, pdy, lddy, pdz or 0, lddz, pdx or 0, lddx, pdw or 0, lddw, pdb or 0, ws or 0, have),
