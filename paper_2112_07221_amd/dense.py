@@ -84,30 +84,43 @@ class Packed:
 
 
 # ---- checks: what the library cannot see from pointers ------------------------------------------------
-# A small call is launches and these lines, so they ask torch for each property once.
+# A small call is launches and these lines, so they ask torch for each property once (and for a tensor's class only where something is wrong:
+# torch.Tensor's isinstance is slow).
 def _not_here(t, what):
     if not isinstance(t, _tensor) or not t.is_cuda:
         raise TypeError(f"{what} must be a tensor on the GPU")
     raise ValueError(f"{what} is on another device than the current one")
 
 
-def _here(t, what):
-    """The current device, which `t` has to be on."""
-    if isinstance(t, Packed):
-        t = t.q
-    if not isinstance(t, _tensor) or not t.is_cuda:
-        raise TypeError(f"{what} must be on the GPU")
-    dev = _current_device()
-    if t.get_device() != dev:
+def _first(t, what):
+    """(pointer, row distance, type, rows, dim, current device) of the matrix that says how large a call is."""
+    try:
+        dev = t.get_device()
+        kind = _types.get(t.dtype)
+        shape = t.shape
+    except AttributeError:
+        raise TypeError(f"{what} must be a matrix on the GPU") from None
+    if dev < 0 or dev != _current_device():
         _not_here(t, what)
-    return dev
+    if kind is None:
+        raise TypeError(f"{what} must be float32, bfloat16 or float16")
+    if len(shape) != 2:
+        raise TypeError(f"{what} must be a matrix")
+    rows, dim = shape
+    ld, along = t.stride()
+    if along != 1 and dim > 1:
+        raise ValueError(f"the values of a row of {what} must lie side by side")
+    return t.data_ptr(), ld if rows > 1 or ld > dim else dim, kind, rows, dim, dev
 
 
 def _matrix(t, what, rows, dim, dev, dtype=None):
     """(pointer, row distance, type) of a [rows, dim] matrix."""
-    if not isinstance(t, _tensor) or t.get_device() != dev:
-        _not_here(t, what)
-    have = t.dtype
+    try:
+        if t.get_device() != dev:
+            _not_here(t, what)
+        have = t.dtype
+    except AttributeError:
+        raise TypeError(f"{what} must be a matrix on the GPU") from None
     kind = _types.get(have)
     if kind is None or (dtype is not None and have is not dtype):
         raise TypeError(f"{what} must be {dtype or 'float32, bfloat16 or float16'}")
@@ -123,11 +136,14 @@ def _vector(t, what, n, dev):
     """Pointer of a contiguous fp32 vector of n values; None stays None."""
     if t is None:
         return None
-    if not isinstance(t, _tensor) or t.get_device() != dev:
-        _not_here(t, what)
-    if t.dtype is not _f32 or t.numel() != n or not t.is_contiguous():
-        raise TypeError(f"{what} must be a contiguous float32 vector of {n} values")
-    return t.data_ptr()
+    try:
+        if t.get_device() != dev:
+            _not_here(t, what)
+        if t.dtype is _f32 and t.numel() == n and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    raise TypeError(f"{what} must be a contiguous float32 vector of {n} values")
 
 
 def _packed(p, what, rows, dim, dev):
@@ -135,14 +151,16 @@ def _packed(p, what, rows, dim, dev):
     if p is None:
         return None, None
     pitch = -(-dim // PACK_BLOCK) * PACK_BLOCK
-    q, e = p.q, p.e
-    for t in (q, e):
-        if not isinstance(t, _tensor) or t.get_device() != dev:
-            _not_here(t, what)
-    if p.dim != dim or q.dtype is not _torch.int8 or e.dtype is not _torch.uint8 or q.shape != (rows, pitch) or e.shape != (rows, pitch // PACK_BLOCK) or \
-            not q.is_contiguous() or not e.is_contiguous():
-        raise ValueError(f"{what} must be the 8-bit form of a matrix of {rows} rows of {dim} values")
-    return q.data_ptr(), e.data_ptr()
+    try:
+        q, e = p.q, p.e
+        if q.get_device() != dev or e.get_device() != dev:
+            _not_here(q if q.get_device() != dev else e, what)
+        if p.dim == dim and q.dtype is _torch.int8 and e.dtype is _torch.uint8 and q.shape == (rows, pitch) and e.shape == (rows, pitch // PACK_BLOCK) and \
+                q.is_contiguous() and e.is_contiguous():
+            return q.data_ptr(), e.data_ptr()
+    except AttributeError:
+        raise TypeError(f"{what} must be a Packed") from None
+    raise ValueError(f"{what} must be the 8-bit form of a matrix of {rows} rows of {dim} values")
 
 
 def _stream(stream, dev):
@@ -169,21 +187,11 @@ def _rc(status, what):
         raise HetError(status, what)
 
 
-def _shape(t, what):
-    if isinstance(t, Packed):
-        return t.rows, t.dim
-    if not isinstance(t, _tensor) or t.dim() != 2:
-        raise TypeError(f"{what} must be a matrix on the GPU")
-    return t.shape
-
-
 # ---- the calls ----------------------------------------------------------------------------------------
 def layer_norm(x, gamma, beta, y, mean=None, rstd=None, packed=None, eps=1e-5, stream=None):
     """y = gamma (x - mean) rstd + beta by rows (het_layer_norm).  packed (a Packed or None) keeps the normalised rows in 8 bits."""
     lib = _lib or load()
-    rows, dim = _shape(x, "x")
-    dev = _here(x, "x")
-    px, ldx, tx = _matrix(x, "x", rows, dim, dev)
+    px, ldx, tx, rows, dim, dev = _first(x, "x")
     py, ldy, ty = _matrix(y, "y", rows, dim, dev)
     q, e = _packed(packed, "packed", rows, dim, dev)
     _rc(lib.het_layer_norm(px, tx, ldx, _vector(gamma, "gamma", dim, dev), _vector(beta, "beta", dim, dev), py, ty, ldy,
@@ -201,9 +209,7 @@ def layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, r
     """dx, dgamma and dbeta of layer_norm (het_layer_norm_backward).  x: the input, with mean; or what the forward pass kept (a Packed;
     mean is not looked at).  residual: a gradient added to dx."""
     lib = _lib or load()
-    rows, dim = _shape(dy, "dy")
-    dev = _here(dy, "dy")
-    pdy, lddy, ty = _matrix(dy, "dy", rows, dim, dev)
+    pdy, lddy, ty, rows, dim, dev = _first(dy, "dy")
     pdx, lddx, tx = _matrix(dx, "dx", rows, dim, dev)
     px = q = e = pm = pr = None
     ldx = ldr = 0
@@ -225,9 +231,7 @@ def layer_norm_backward(dy, x, gamma, mean, rstd, dx, dgamma=None, dbeta=None, r
 def pack(x, packed, stream=None):
     """x in 8 bits into `packed` (het_pack)."""
     lib = _lib or load()
-    rows, dim = _shape(x, "x")
-    dev = _here(x, "x")
-    px, ldx, tx = _matrix(x, "x", rows, dim, dev)
+    px, ldx, tx, rows, dim, dev = _first(x, "x")
     q, e = _packed(packed, "packed", rows, dim, dev)
     _rc(lib.het_pack(px, tx, ldx, q, e, rows, dim, _stream(stream, dev)), "het_pack")
 
@@ -235,9 +239,7 @@ def pack(x, packed, stream=None):
 def expand(packed, y, act=ACT_NONE, gamma=None, beta=None, stream=None):
     """y = act(gamma v + beta) of the values v that `packed` holds (het_expand)."""
     lib = _lib or load()
-    rows, dim = _shape(packed, "packed")
-    dev = _here(packed, "packed")
-    py, ldy, ty = _matrix(y, "y", rows, dim, dev)
+    py, ldy, ty, rows, dim, dev = _first(y, "y")
     q, e = _packed(packed, "packed", rows, dim, dev)
     _rc(lib.het_expand(q, e, rows, dim, _vector(gamma, "gamma", dim, dev), _vector(beta, "beta", dim, dev), act, py, ty, ldy, _stream(stream, dev)), "het_expand")
 
@@ -263,11 +265,12 @@ def linear(x, w, bias, y, act=ACT_NONE, residual=None, z=None, workspace=None, s
     """y = act(x w^T + bias) + residual (het_linear).  z keeps x w^T + bias: a tensor of x's type, or a Packed.  y and residual have
     x's type, or are float32."""
     lib = _lib or load()
-    rows, inp = _shape(x, "x")
-    out = _shape(w, "w")[0]
-    dev = _here(x, "x")
-    px, ldx, kind = _matrix(x, "x", rows, inp, dev)
-    pw, ldw, _ = _matrix(w, "w", out, inp, dev, x.dtype)
+    px, ldx, kind, rows, inp, dev = _first(x, "x")
+    pw, ldw, w_kind, out, w_inp, _ = _first(w, "w")
+    if w_kind != kind:
+        raise TypeError(f"w must be {x.dtype}")
+    if w_inp != inp:
+        raise ValueError(f"w must have rows of {inp} values")
     py, ldy, y_kind = _matrix(y, "y", rows, out, dev)
     pr = pz = zq = ze = None
     ldr = ldz = 0
@@ -286,16 +289,12 @@ def linear_backward(dy, x, w, z, act, dz, dx, dw, dbias=None, x_act=ACT_NONE, x_
     """dz = dy act'(z), dbias, dx = dz w and dw = dz^T x (het_linear_backward); each of dx, dw and dbias may be None.  z and x: tensors, or
     what the forward pass kept (a Packed); an x so kept stands for x_act(x_gamma v + x_beta).  dz may be None where it would be dy."""
     lib = _lib or load()
-    rows, out = _shape(dy, "dy")
+    pdy, lddy, y_kind, rows, out, dev = _first(dy, "dy")
     ref = w if w is not None else dw
     if ref is None:
         raise ValueError("w or dw says how wide the layer's input is")
-    inp, dtype = _shape(ref, "w")[1], ref.dtype
-    kind = _types.get(dtype)
-    if kind is None:
-        raise TypeError("w must be float32, bfloat16 or float16")
-    dev = _here(dy, "dy")
-    pdy, lddy, y_kind = _matrix(dy, "dy", rows, out, dev)
+    _, _, kind, _, inp, _ = _first(ref, "w")
+    dtype = ref.dtype
     px = pxq = pxe = pg = pb = pw = pz = pzq = pze = pdz = pdx = pdw = None
     ldx = ldw = ldz = lddz = lddx = lddw = 0
     if dz is not None:
