@@ -103,7 +103,7 @@ ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bo
     double best = 1e30;
     for (int tile = 256; tile >= 128; tile /= 2) {
         const int64_t tiles = ((m + tile - 1) / tile) * ((n + tile - 1) / tile);
-        for (int64_t splits = 1; splits <= 32 && (splits == 1 || (splits * 4 <= steps && tiles * splits <= 2 * CUS)); ++splits) {
+        for (int64_t splits = 1; splits <= 32 && (splits == 1 || (splits * 4 <= steps && tiles * splits <= 4 * CUS)); ++splits) {
             const double us = tiles_us(tile, tiles, splits, steps, m, n, f32);
             if (us < best) { best = us; p.tile = tile; p.splits = (int)splits; }
         }
