@@ -353,7 +353,7 @@ class ResidualBlock:
         self.db1, self.db2 = new(hidden), new(dim)
         # between the passes
         self._h, self._u = new(rows, dim, dtype=dtype), new(rows, hidden, dtype=dtype)
-        self._mean, self._rstd, self._x = new(rows), new(rows), None
+        self._mean, self._rstd, self._x, self._ready = new(rows), new(rows), None, False
         self._n8 = Packed.empty(rows, dim, device) if keep8 else None
         self._z = Packed.empty(rows, hidden, device) if keep8 else new(rows, hidden, dtype=dtype)
         # backward (the forward pass' h and u are free by then if they were kept in 8 bits)
@@ -372,11 +372,14 @@ class ResidualBlock:
         layer_norm(x, self.gamma, self.beta, self._h, self._mean, self._rstd, packed=self._n8, eps=self.eps)
         linear(self._h, self.w1, self.b1, self._u, self.act, z=self._z, workspace=self._workspace)
         linear(self._u, self.w2, self.b2, y, residual=x, workspace=self._workspace)
-        self._x = None if self.keep8 else x
+        self._x, self._ready = None if self.keep8 else x, True
 
     def backward(self, dy, dx):
         """dx and the parameters' gradients from dy (float32 [rows, dim]), once for a forward pass.  dx may be dy itself."""
         keep8 = self.keep8
+        if not self._ready:
+            raise RuntimeError("backward follows a forward pass")
+        self._ready = False
         linear_backward(dy, self._z if keep8 else self._u, self.w2, None, ACT_NONE, self._dz2, self._du, self.dw2, self.db2,
                         x_act=self.act if keep8 else ACT_NONE, workspace=self._workspace)
         # dz1 takes du's place: slope and product follow each other

@@ -394,7 +394,7 @@ def test_expand_through_weights_and_activation(rows, dim, affine, act, t):
 # sums over few tiles (split); widths of one
 LINEAR_SHAPES = [(1, 1, 1), (1, 64, 16), (1, 1664, 33), (2, 7, 5), (8, 130, 40), (16, 64, 32), (17, 96, 31), (33, 200, 65), (64, 72, 48), (65, 64, 128), (100, 33, 17),
                  (128, 128, 128), (129, 65, 127), (200, 31, 260), (130, 640, 129), (257, 1001, 70), (66, 3000, 130), (384, 192, 256), (300, 8, 300), (520, 320, 264),
-                 (700, 2000, 640), (640, 4200, 1030)]
+                 (700, 2000, 640), (640, 4200, 1030), (300, 8200, 200)]
 LINEAR_TYPES = [(F32, F32), (BF16, BF16), (F16, F16), (BF16, F32), (F16, F32)]
 
 
@@ -482,6 +482,47 @@ def test_linear_backward(rows, inp, out, t, ty, kept):
         dense.linear_backward(same, None, w, None, dense.ACT_NONE, None, a, None)
         dense.linear_backward(same, None, w, None, dense.ACT_NONE, same, b, None, db)
         assert torch.equal(a, b) and torch.equal(same, dy)
+
+
+def test_the_shapes_reach_split_sums():
+    """(300, 8200, 200) is added up from splits (bias, residual, kept z and activation come behind them), forward and in dw's long sum over rows."""
+    assert dense.linear_workspace(300, 8200, 200, BF16) > 0
+    assert dense.linear_workspace(30000, 256, 200, BF16, backward=True, dx=False, dbias=False) > 0
+
+
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,inp,out", [(4113, 136, 3592), (4113, 3592, 136), (136, 3592, 4112), (30000, 256, 200)])
+def test_large_tiles_and_long_sums(rows, inp, out, t):
+    """Sizes at which the large tiles are taken, with edges, and sums over many rows; the reference in 64 bits on the GPU (contiguous operands)."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows + inp + out)
+    x, w = torch.randn(rows, inp, generator=g, device="cuda").to(t), (torch.randn(out, inp, generator=g, device="cuda") / math.sqrt(inp)).to(t)
+    bias, r, dy = torch.randn(out, generator=g, device="cuda"), torch.randn(rows, out, generator=g, device="cuda"), torch.randn(rows, out, generator=g, device="cuda").to(t)
+    y, p = Guarded(rows, out, F32), dense.Packed.empty(rows, out)
+    dense.linear(x, w, bias, y.m, dense.ACT_RELU, residual=r, z=p)
+
+    def within(got, want, tol, what):
+        off = (got.double() - want).abs()
+        assert bool((off <= tol).all()), (what, float((off - tol).max()))
+
+    wt = w.double().t().contiguous()
+    z = torch.mm(x.double(), wt) + bias.double()
+    z_off = (2 * (inp + 1) + 2) * U * torch.mm(x.double().abs(), wt.abs()) + 2 * U * z.abs()
+    want = z.clamp(min=0) + r.double()
+    within(y.m, want, z_off + 2 * U * want.abs(), "y")
+    assert y.untouched()
+    step = torch.exp2(p.e.double() - 127).repeat_interleave(32, 1)
+    within((p.q.double() * step)[:, :out], z, (step / 2)[:, :out] + z_off, "z in 8 bits")
+    dz, dx, dw, db = torch.empty(rows, out, dtype=t, device="cuda"), Guarded(rows, inp, t), Guarded(out, inp, t), torch.empty(out, device="cuda")
+    dense.linear_backward(dy, x, w, p, dense.ACT_RELU, dz, dx.m, dw.m, db)
+    assert torch.equal(dz, torch.where(p.q[:, :out] > 0, dy, torch.zeros((), dtype=t, device="cuda")))
+    d = dz.double()
+    for got, a, b, what in ((dx, d, w.double(), "dx"), (dw, d.t().contiguous(), x.double(), "dw")):
+        v = torch.mm(a, b)
+        o = (2 * a.shape[1] + 2) * U * torch.mm(a.abs(), b.abs())
+        within(got.m, v, o + H(t) * (v.abs() + o) + tiny(t), what)
+        assert got.untouched()
+    within(db, d.sum(0), rows * U * d.abs().sum(0), "dbias")
 
 
 def test_linear_gradient_against_differences():

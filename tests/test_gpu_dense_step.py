@@ -134,3 +134,5 @@ def test_the_gradient_may_take_the_place_of_the_outputs():
     b.forward(x, y)
     b.backward(dy, dy)
     assert torch.equal(dx, dy)
+    with pytest.raises(RuntimeError):                     # once for a forward pass
+        b.backward(dy, dx)
