@@ -99,7 +99,9 @@ __device__ __forceinline__ int col_of(int i) { return 16 * ((i >> 2) & 1) + 4 * 
 
 // An operand's tile in LDS: R rows and 128 bytes of k.
 //   K:  [row][128 bytes], pieces of 16 bytes;  across:  [k][R values].
-// The order of the pieces within 128 (or 64 R / 32 ...) bytes is mixed by row or k, so that the lanes of a read meet all banks.
+// The order of a row's pieces is mixed by the row's (or k's) number, so that the 16 lanes whose 16 bytes are read at a time meet all 64 banks: rows
+// of 128 bytes two by two, and of the permuted operand the rows that col_of brings together.  (Mixed by the last three bits, as 32 banks would
+// want it, half of the reads conflicted: 2.5e7 cycles in 8192 x 4096 -> 4096; now none do.)
 template <typename T, int R, bool K, bool PERMUTED>
 struct Tile {
     static constexpr int PIECE = 16 / (int)sizeof(T);             // values of a piece
@@ -159,7 +161,7 @@ __device__ __forceinline__ int tile_of(int block, int tiles)
 // Tiles in bands of 8 rows of tiles: neighbours share A's rows or B's.
 __device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int &tm, int &tn)
 {
-    const int band = t / (8 * tiles_n), first = band * 8, high = tiles_m - first < 8 ? tiles_m - first  : 8, in = t - band * 8 * tiles_n;
+    const int band = t / (8 * tiles_n), first = band * 8, high = tiles_m - first < 8 ? tiles_m - first : 8, in = t - band * 8 * tiles_n;
     tm = first + in % high;
     tn = in / high;
 }
@@ -327,7 +329,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
     };
     // A frag's reads go out before the products of the frag before.  The last frag of a step is in registers before its products start: at that point
     // the buffer is free for the step after the next, and the next step's first frag can be read.  The copies of one operand go out among those
-    // last products, the other's among the first ones of the next step: all sixteen at once held the products up (8192 x 4096 -> 4096 bf16: dw 231 -> 216 us).
+    // last products, the other's among the first ones of the next step: all of them at once held the products up (8192 x 4096 -> 4096 bf16: dw 231 -> 216 us).
     int left = k_end - k_begin;
     auto step = [&](i32x4 *la, i32x4 *lb, i32x4 *next_a, i32x4 *next_b) {
         read(la, lb, 1, 1);
@@ -375,9 +377,11 @@ __global__ __launch_bounds__(256) void lay_kernel(const U *p, int64_t ld, int64_
 {
     constexpr int PIECE = 16 / (int)sizeof(U);
     const int per = pitch / PIECE;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+    int64_t row;
+    int at;
+    row_and_piece((int64_t)blockIdx.x * 256 + threadIdx.x, per, row, at);
     if (row >= rows) return;
-    const int at = (int)(i - row * per) * PIECE;
+    at *= PIECE;
     const U *from = p + row * ld;
     vec<U, PIECE> v = {};
     if (at + PIECE <= width) {
@@ -394,9 +398,11 @@ template <typename T>
 __global__ __launch_bounds__(256) void join_kernel(ProductArgs a)
 {
     const int width = partial_width(a.n), per = (a.n + PACK_BLOCK - 1) / PACK_BLOCK * 4;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+    int64_t row;
+    int c;
+    row_and_piece((int64_t)blockIdx.x * 256 + threadIdx.x, per, row, c);
     if (row >= a.m) return;
-    const int c = (int)(i - row * per), col = c * CHUNK, n = a.n - col;
+    const int col = c * CHUNK, n = a.n - col;
     f32x8 v = {};
     if (n > 0) {
         const float *p = a.partial + row * width + col;

@@ -393,9 +393,11 @@ template <typename T>
 __global__ __launch_bounds__(256) void pack_kernel(PackArgs a)
 {
     const int per = a.pitch / CHUNK;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+    int64_t row;
+    int c;
+    row_and_piece((int64_t)blockIdx.x * 256 + threadIdx.x, per, row, c);
     if (row >= a.rows) return;                      // (whole blocks: a row has four lanes or a multiple)
-    const int c = (int)(i - row * per), n = chunk_values(c, a.dim);
+    const int n = chunk_values(c, a.dim);
     const f32x8 v = n > 0 ? load_some(static_cast<const T *>(a.x) + row * a.ldx + c * CHUNK, n) : f32x8{};
     pack_chunk(a.q + row * a.pitch, a.e + row * (a.pitch / PACK_BLOCK), c, v);
 }
@@ -421,9 +423,11 @@ template <typename T>
 __global__ __launch_bounds__(256) void expand_kernel(ExpandArgs a)
 {
     const int per = (a.dim + CHUNK - 1) / CHUNK;
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, row = i / per;
+    int64_t row;
+    int c;
+    row_and_piece((int64_t)blockIdx.x * 256 + threadIdx.x, per, row, c);
     if (row >= a.rows) return;
-    const int c = (int)(i - row * per), n = chunk_values(c, a.dim);
+    const int n = chunk_values(c, a.dim);
     uint64_t q;
     __builtin_memcpy(&q, a.q + row * a.pitch + c * CHUNK, 8);
     f32x8 v = unpack_chunk(q, a.e[row * (a.pitch / PACK_BLOCK) + (c >> 2)]);

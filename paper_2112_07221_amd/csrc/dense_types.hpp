@@ -20,6 +20,13 @@ constexpr int CHUNK = 8;             // elements a lane handles at a time in the
 constexpr int PACK_BLOCK = 32;       // values that share a step in the 8-bit form
 constexpr uint32_t PACK_NOT_FINITE = 255;
 
+// Which of a row's `per` pieces thread `i` of a launch of a piece a thread has.  (A division of 64 bits is some eighty instructions.)
+__device__ __forceinline__ void row_and_piece(int64_t i, int per, int64_t &row, int &piece)
+{
+    if ((uint64_t)i >> 32) { row = i / per; piece = (int)(i - row * per); }
+    else { row = (uint32_t)i / (uint32_t)per; piece = (int)((uint32_t)i - (uint32_t)row * (uint32_t)per); }
+}
+
 // ---- pieces of rows at any alignment ------------------------------------------------------------------
 // Rows may begin at any element (odd widths, wider matrices), and the vector memory path takes any address: a piece is one load
 // of 16 bytes (two for fp32) whatever its alignment, and no second set of kernels is needed for odd strides.
