@@ -33,36 +33,34 @@ struct ProductArgs {
 
 __device__ __forceinline__ int partial_width(int n) { return (n + 15) & ~15; }
 
-template <typename TY>
-__device__ __forceinline__ void finish_store(const Finish &f, int64_t row, int col, int n, f32x8 v)
-{
-    if (f.residual) {
-        const f32x8 r = load_some(static_cast<const TY *>(f.residual) + row * f.ldr + col, n);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += r[j];
-    }
-    store_some(static_cast<TY *>(f.y) + row * f.ldy + col, v, n);
-}
-
-// z of a chunk at (row, col), n of its values in the matrix.  Values behind the row's end are zero.
-__device__ __forceinline__ f32x8 finish_bias(const Finish &f, int col, int n, f32x8 v)
-{
-    if (f.bias && n > 0) {
-        const f32x8 b = load_some(f.bias + col, n);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += b[j];
-    }
-    return v;
-}
-
+// The n values of bias and residual that belong to a chunk at (row, col); zero behind the row's end and where there are none.
+__device__ __forceinline__ f32x8 finish_bias(const Finish &f, int col, int n) { return f.bias && n > 0 ? load_some(f.bias + col, n) : f32x8{}; }
 template <typename T>
-__device__ __forceinline__ void finish_value(const Finish &f, int64_t row, int col, int n, f32x8 v)
+__device__ __forceinline__ f32x8 finish_residual(const Finish &f, int64_t row, int col, int n)
+{
+    if (!f.residual || n <= 0) return f32x8{};
+    const int64_t at = row * f.ldr + col;
+    return f.y_f32 ? load_some(static_cast<const float *>(f.residual) + at, n) : load_some(static_cast<const T *>(f.residual) + at, n);
+}
+
+// Ends z of that chunk.
+template <typename T>
+__device__ __forceinline__ void finish_value(const Finish &f, int64_t row, int col, int n, f32x8 v, f32x8 residual)
 {
     if (n <= 0) return;
     if (f.z) store_some(static_cast<T *>(f.z) + row * f.ldz + col, v, n);
     v = act_chunk<false>(f.act, v);
-    if (f.y_f32) finish_store<float>(f, row, col, n, v);
-    else finish_store<T>(f, row, col, n, v);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += residual[j];
+    if (f.y_f32) store_some(static_cast<float *>(f.y) + row * f.ldy + col, v, n);
+    else store_some(static_cast<T *>(f.y) + row * f.ldy + col, v, n);
+}
+
+__device__ __forceinline__ f32x8 plus(f32x8 a, f32x8 b)
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) a[j] += b[j];
+    return a;
 }
 
 // ---- operands in LDS ------------------------------------------------------------------------------------
@@ -233,9 +231,9 @@ __device__ __forceinline__ void finish_tile(const ProductArgs &a, int split, int
         for (int it = 0; it < 4; ++it) {
             const int r = 8 * it + lane / 8, row = row0 + r, n = a.n - col;
             if (row >= a.m) return;
-            const f32x8 v = finish_bias(a.f, col, n, sums(r));
+            const f32x8 v = plus(sums(r), finish_bias(a.f, col, n));
             if (a.f.q) pack_chunk(a.f.q + (int64_t)row * a.f.pitch, a.f.e + (int64_t)row * (a.f.pitch / PACK_BLOCK), col / CHUNK, v);
-            finish_value<T>(a.f, row, col, n, v);
+            finish_value<T>(a.f, row, col, n, v, finish_residual<T>(a.f, row, col, n));
         }
     }
 }
@@ -403,6 +401,7 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a)
     row_and_piece((int64_t)blockIdx.x * 256 + threadIdx.x, per, row, c);
     if (row >= a.m) return;
     const int col = c * CHUNK, n = a.n - col;
+    const f32x8 bias = finish_bias(a.f, col, n), residual = finish_residual<T>(a.f, row, col, n);
     f32x8 v = {};
     if (n > 0) {
         const float *p = a.partial + row * width + col;
@@ -412,9 +411,9 @@ __global__ __launch_bounds__(256) void join_kernel(ProductArgs a)
             for (int j = 0; j < 8; ++j) v[j] += x[j];
         }
     }
-    v = finish_bias(a.f, col, n, v);
+    v = plus(v, bias);
     if (a.f.q) pack_chunk(a.f.q + row * a.f.pitch, a.f.e + row * (a.f.pitch / PACK_BLOCK), c, v);
-    finish_value<T>(a.f, row, col, n, v);
+    finish_value<T>(a.f, row, col, n, v, residual);
 }
 
 // ---- few rows, or small products --------------------------------------------------------------------------
@@ -475,6 +474,10 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void product_small_kernel(Product
     __shared__ float lds[SMALL_WAVES][16 * MT][16 * NT + 4];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
     const int row0 = blockIdx.x / a.tiles_n * 16 * MT, col0 = blockIdx.x % a.tiles_n * 16 * NT;
+    // the chunk this thread ends, and what is added to it, asked for ahead
+    const int c = threadIdx.x % (2 * NT), at = threadIdx.x / (2 * NT), row = row0 + at, col = col0 + c * CHUNK, n = a.n - col;
+    const bool ends = at < 16 * MT && row < a.m;
+    const f32x8 bias = ends ? finish_bias(a.f, col, n) : f32x8{}, residual = ends ? finish_residual<T>(a.f, row, col, n) : f32x8{};
     f32x4 acc[MT][NT] = {};
     auto products = [&](const typename DA::F *fa, const typename DB::F *fb) {
 #pragma unroll
@@ -494,7 +497,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void product_small_kernel(Product
         typename DB::F fb[AHEAD][2][NT];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
-            const int at = t + u * SMALL_WAVES, k = (at < whole ? at : t) * SPAN + 2 * g * DA::PIECE;
+            const int span = t + u * SMALL_WAVES, k = (span < whole ? span : t) * SPAN + 2 * g * DA::PIECE;
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
 #pragma unroll
@@ -525,9 +528,7 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void product_small_kernel(Product
 #pragma unroll
         for (int j = 0; j < NT; ++j) *reinterpret_cast<f32x4 *>(&lds[wave][16 * i + r][16 * j + 4 * g]) = acc[i][j];
     __syncthreads();
-    const int c = threadIdx.x % (2 * NT), at = threadIdx.x / (2 * NT), row = row0 + at;
-    if (at >= 16 * MT || row >= a.m) return;
-    const int col = col0 + c * CHUNK, n = a.n - col;
+    if (!ends) return;
     f32x8 v = {};
 #pragma unroll
     for (int w = 0; w < SMALL_WAVES; ++w)
@@ -535,9 +536,9 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void product_small_kernel(Product
         for (int j = 0; j < 8; ++j) v[j] += lds[w][at][c * CHUNK + j];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = j < n ? v[j] : 0.f;
-    v = finish_bias(a.f, col, n, v);
+    v = plus(v, bias);
     if (NT == 2 && a.f.q) pack_chunk(a.f.q + (int64_t)row * a.f.pitch, a.f.e + (int64_t)row * (a.f.pitch / PACK_BLOCK), col / CHUNK, v);
-    finish_value<T>(a.f, row, col, n, v);
+    finish_value<T>(a.f, row, col, n, v, residual);
 }
 
 } // namespace het
