@@ -166,20 +166,6 @@ __device__ __forceinline__ void tile_at(int t, int tiles_m, int tiles_n, int &tm
 
 // Outputs and residuals pass the L2, which holds the operands that neighbouring tiles share (4096 x 1664 -> 4096 with gelu and z in 8 bits 72.5 -> 70.5 us
 // with its expansion).
-template <typename V>
-__device__ __forceinline__ void store_past(void *p, V v)
-{
-    typedef int32_t any16 __attribute__((ext_vector_type(4), aligned(2)));
-    static_assert(sizeof(V) == 16, "a piece");
-    __builtin_nontemporal_store(__builtin_bit_cast(i32x4, v), static_cast<any16 *>(p));
-}
-template <typename V>
-__device__ __forceinline__ V load_past(const void *p)
-{
-    typedef int32_t any16 __attribute__((ext_vector_type(4), aligned(2)));
-    static_assert(sizeof(V) == 16, "a piece");
-    return __builtin_bit_cast(V, __builtin_nontemporal_load(static_cast<const any16 *>(p)));
-}
 
 // Four chunks at `col` of the rows row, row + 8, ... of 16-bit outputs, or of any with z kept; sums(r): the chunk of row r of the 32.
 template <typename T, typename TY, typename S>

@@ -124,7 +124,7 @@ __global__ __launch_bounds__(MOST) void norm_kernel(NormArgs a)
         const f32x8 b = a.beta ? load_row<WHOLE>(a.beta, c, dim) : f32x8{};
 #pragma unroll
         for (int j = 0; j < 8; ++j) h[j] = h[j] * g[j] + b[j];
-        store_row<WHOLE>(y, c, dim, h);
+        store_row<WHOLE, true>(y, c, dim, h);         // (past the L2: 106496 x 64 to bf16 and 8 bits, expanded, 17.0 -> 16.3 us)
     }
 }
 

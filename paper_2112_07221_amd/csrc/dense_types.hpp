@@ -46,6 +46,22 @@ __device__ __forceinline__ void store_chunk(T *p, f32x8 f)
     __builtin_memcpy(p, &v, sizeof(v));
 }
 
+// 16 bytes that are not kept in the L2.
+template <typename V>
+__device__ __forceinline__ void store_past(void *p, V v)
+{
+    typedef int32_t any16 __attribute__((ext_vector_type(4), aligned(2)));
+    static_assert(sizeof(V) == 16, "a piece");
+    __builtin_nontemporal_store(__builtin_bit_cast(i32x4, v), static_cast<any16 *>(p));
+}
+template <typename V>
+__device__ __forceinline__ V load_past(const void *p)
+{
+    typedef int32_t any16 __attribute__((ext_vector_type(4), aligned(2)));
+    static_assert(sizeof(V) == 16, "a piece");
+    return __builtin_bit_cast(V, __builtin_nontemporal_load(static_cast<const any16 *>(p)));
+}
+
 // The first `n` (0 .. 8) of a chunk; the others read as zero and are not written.
 template <typename T>
 __device__ __forceinline__ f32x8 load_some(const T *p, int n)
@@ -95,10 +111,13 @@ __device__ __forceinline__ f32x8 raw_values(vec<T, 8> v, int c, int dim)
 }
 template <bool WHOLE, typename T>
 __device__ __forceinline__ f32x8 load_row(const T *row, int c, int dim) { return raw_values<WHOLE>(load_raw<WHOLE>(row, c, dim), c, dim); }
-template <bool WHOLE, typename T>
+template <bool WHOLE, bool PAST = false, typename T>
 __device__ __forceinline__ void store_row(T *row, int c, int dim, f32x8 f)
 {
     const int n = dim - c * CHUNK;
+    if constexpr (PAST && sizeof(T) == 2) {
+        if (WHOLE ? n > 0 : n >= CHUNK) { store_past(row + c * CHUNK, __builtin_convertvector(f, vec<T, 8>)); return; }
+    }
     if (WHOLE ? n > 0 : n >= CHUNK) store_chunk(row + c * CHUNK, f);
     else if (!WHOLE && n > 0) store_some(row + c * CHUNK, f, n);
 }
