@@ -132,10 +132,8 @@ __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f
 // and the polynomial stays where it is): Phi is off by at most 3.2e-7, v Phi(v) by 2.1e-7.  The tail is formed itself, not as 1 - erf, so no digits are
 // lost for negative v.  One exponential, six multiply-adds: with the math library's erf and exp slope_kernel took 58.2 us for 8192 x 4096 values
 // (bf16, z in 8 bits; memory's share is 33), with the rational approximation 7.1.26 of Abramowitz and Stegun 40.0.
-__device__ __forceinline__ float normal_exponent(float v) { return v * -0.72134752044448170f * v; }        // log2 exp(-v^2 / 2)
-__device__ __forceinline__ float normal_tail(float v)
+__device__ __forceinline__ float normal_tail(float v, float x)           // x: |v|, at most 7
 {
-    const float x = fminf(fabsf(v), 7.f);
     float q = 2.8578077035490423e-05f;
     q = fmaf(q, x, -0.0007268775952979922f);
     q = fmaf(q, x, 0.007932470180094242f);
@@ -143,14 +141,15 @@ __device__ __forceinline__ float normal_tail(float v)
     q = fmaf(q, x, 0.26238641142845154f);
     q = fmaf(q, x, -1.151138186454773f);
     q = fmaf(q, x, -0.9999993443489075f);
-    return __builtin_amdgcn_exp2f(normal_exponent(v) + q);
+    return __builtin_amdgcn_exp2f(fmaf(v * -0.72134752044448170f, v, q));
 }
+__device__ __forceinline__ float within_seven(float v) { return __builtin_amdgcn_fmed3f(fabsf(v), 0.f, 7.f); }
 
 __device__ __forceinline__ float act_value(int act, float v)
 {
     switch (act) {
     case DENSE_ACT_RELU: return v > 0.f ? v : v == v ? 0.f : v;                       // NaN stays NaN
-    case DENSE_ACT_GELU: { const float tail = normal_tail(v); return v * (v < 0.f ? tail : 1.f - tail); }
+    case DENSE_ACT_GELU: { const float x = within_seven(v); return fmaf(-x, normal_tail(v, x), fmaxf(v, 0.f)); }      // (7 times the tail of what is beyond: 0)
     case DENSE_ACT_SILU: return v * __builtin_amdgcn_rcpf(1.f + exp_of(-v));
     default: return v;
     }
@@ -161,8 +160,8 @@ __device__ __forceinline__ float act_slope(int act, float v)
     switch (act) {
     case DENSE_ACT_RELU: return v > 0.f ? 1.f : v == v ? 0.f : v;
     case DENSE_ACT_GELU: {
-        const float tail = normal_tail(v);
-        return fmaf(v * 0.39894228040143268f, __builtin_amdgcn_exp2f(normal_exponent(v)), v < 0.f ? tail : 1.f - tail);
+        const float tail = normal_tail(v, within_seven(v)), bell = __builtin_amdgcn_exp2f(v * -0.72134752044448170f * v);
+        return fmaf(v * 0.39894228040143268f, bell, v < 0.f ? tail : 1.f - tail);
     }
     case DENSE_ACT_SILU: { const float p = __builtin_amdgcn_rcpf(1.f + exp_of(-v)); return p * (1.f + v * (1.f - p)); }
     default: return 1.f;
