@@ -90,17 +90,26 @@ bool linear_sizes(const het_linear_t *l)
            l->rows * std::max(l->in, l->out) <= MOST_VALUES;
 }
 
-template <typename T, typename TY>
-void launch_slope(const SlopeArgs &s, dim3 grid, hipStream_t st)
-{
-    if (s.dim % CHUNK == 0) slope_kernel<T, TY, true><<<grid, 256, 0, st>>>(s);
-    else slope_kernel<T, TY, false><<<grid, 256, 0, st>>>(s);
-}
-
+// Workgroups down the rows: one where they are few, else enough to fill the chip, a turn of rows for each at least.
 int slope_splits(int64_t rows, int32_t out)
 {
-    // enough workgroups to fill the chip, a turn of rows for each at least
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)PARTIALS, cdiv(rows, 8 * SLOPE_ROWS), cdiv(2048, cdiv(out, SLOPE_COLS))}));
+    if (rows <= SLOPE_ALONE_ROWS) return 1;
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)PARTIALS, cdiv(rows, SLOPE_THREADS / SLOPE_ACROSS * SLOPE_ROWS), cdiv(2048, cdiv(out, SLOPE_ACROSS * CHUNK))}));
+}
+
+template <typename T, typename TY>
+void launch_slope(const SlopeArgs &s, int splits, hipStream_t st)
+{
+    const bool whole = s.dim % CHUNK == 0;
+    if (splits == 1) {
+        const uint32_t grid = (uint32_t)cdiv(s.dim, SLOPE_ALONE_ACROSS * CHUNK);
+        if (whole) slope_kernel<T, TY, true, SLOPE_ALONE_THREADS, SLOPE_ALONE_ACROSS><<<grid, SLOPE_ALONE_THREADS, 0, st>>>(s);
+        else slope_kernel<T, TY, false, SLOPE_ALONE_THREADS, SLOPE_ALONE_ACROSS><<<grid, SLOPE_ALONE_THREADS, 0, st>>>(s);
+        return;
+    }
+    const dim3 grid((uint32_t)cdiv(s.dim, SLOPE_ACROSS * CHUNK), (uint32_t)splits);
+    if (whole) slope_kernel<T, TY, true, SLOPE_THREADS, SLOPE_ACROSS><<<grid, SLOPE_THREADS, 0, st>>>(s);
+    else slope_kernel<T, TY, false, SLOPE_THREADS, SLOPE_ACROSS><<<grid, SLOPE_THREADS, 0, st>>>(s);
 }
 
 // Where a call's scratch lies in its workspace, from 0 on in order, each piece at a multiple of 16 bytes.
@@ -147,7 +156,7 @@ BackPlan back_plan(const het_linear_t *l)
     p.ldx = l->xq ? laid_pitch(l->in, l->type) : l->ldx;
     if (l->dw) p.dw = product_plan(l->out, l->in, l->rows, l->type, false, false, dz_lies, l->xq || product_lies(l->x, l->ldx, l->in, l->type));
     p.lay_dz = p.dx.lay_a || p.dw.lay_a;
-    p.bias_at = room.take(l->dbias ? (int64_t)p.slope * width_of(l->out) * 4 : 0);
+    p.bias_at = room.take(l->dbias && p.slope > 1 ? (int64_t)p.slope * width_of(l->out) * 4 : 0);
     p.partial_at = room.take(std::max(p.dx.partial_bytes, p.dw.partial_bytes));
     p.dz_at = room.take_laid(p.lay_dz, l->rows, l->out, l->type);
     p.w_at = room.take_laid(p.dx.lay_b, l->out, l->in, l->type);
@@ -286,11 +295,12 @@ int het_linear_backward(const het_linear_t *l, void *hip_stream)
         s.z = l->z; s.ldz = l->ldz; s.q = l->zq; s.e = l->ze;
         s.dz = l->dz; s.lddz = l->lddz;
         if (p.lay_dz) { laid = s.laid = ws + p.dz_at; ld_laid = s.laid_pitch = laid_pitch(l->out, l->type); }
-        s.partial = l->dbias ? reinterpret_cast<float *>(ws + p.bias_at) : nullptr;
+        const bool alone = p.slope == 1;
+        s.sums = !l->dbias ? nullptr : alone ? l->dbias : reinterpret_cast<float *>(ws + p.bias_at);
+        s.sums_width = alone ? l->out : width_of(l->out);
         s.rows = l->rows; s.dim = l->out; s.pitch = pitch_of(l->out); s.act = l->act;
-        const dim3 grid((uint32_t)cdiv(l->out, SLOPE_COLS), (uint32_t)p.slope);
-        with_types(l->y_type, l->type, [&](auto ty, auto t) { launch_slope<typename decltype(t)::type, typename decltype(ty)::type>(s, grid, st); });
-        if (l->dbias) launch_column_sum(s.partial, p.slope, 1, l->out, l->dbias, nullptr, st);
+        with_types(l->y_type, l->type, [&](auto ty, auto t) { launch_slope<typename decltype(t)::type, typename decltype(ty)::type>(s, p.slope, st); });
+        if (l->dbias && !alone) launch_column_sum(s.sums, p.slope, 1, l->out, l->dbias, nullptr, st);
     } else if (p.lay_dz) {
         lay(laid, ld_laid, l->rows, l->out, ws + p.dz_at, l->type, st);
     }

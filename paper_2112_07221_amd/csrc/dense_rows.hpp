@@ -307,36 +307,41 @@ static __global__ __launch_bounds__(COLUMN_THREADS) void column_sum_kernel(Colum
 
 // ---- the slope of the activation and the bias' gradient -------------------------------------------------
 // dz = dy act'(z), handed on in the layer's type (the matrix instructions take it so); dbias = column sums of dz before that rounding.
-// A thread holds 8 columns and goes down the rows; 32 of them side by side, 8 below each other, and the partial sums as above.
+// A thread holds 8 columns and goes down the rows.
 struct SlopeArgs {
     const void *dy, *z;
     const int8_t *q;         // z in 8 bits; null: z, or no activation
     const uint8_t *e;
     void *dz;
     void *laid;              // dz once more, as product_kernel takes it, or null
-    float *partial;          // null: no bias
+    float *sums;             // column sums, [workgroups down][sums_width]; null: no bias
     int64_t lddy, ldz, lddz, laid_pitch, rows;
-    int dim, pitch, act;
+    int dim, pitch, act, sums_width;
 };
 
-constexpr int SLOPE_COLS = 32 * CHUNK;
+// Many rows: 32 threads beside each other and 8 below, partial sums of many workgroups.  Few rows: one workgroup goes down all of them, 8 threads
+// beside each other and 128 below, and ends the sums itself: no second launch (100 x 4096: 4.7 us; 512 x 512 9.1 and 1001 x 250 21.2, bound by the
+// slope's arithmetic on so few compute units, where workgroups down the rows and the second launch take 5.9 + 3.0).
+constexpr int SLOPE_ACROSS = 32, SLOPE_THREADS = 256, SLOPE_ALONE_ACROSS = 8, SLOPE_ALONE_THREADS = 1024;
 constexpr int SLOPE_ROWS = 2;              // rows a thread has in flight
+constexpr int64_t SLOPE_ALONE_ROWS = 256;  // one turn of them
 
-template <typename T, typename TY, bool WHOLE>
-__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
+template <typename T, typename TY, bool WHOLE, int THREADS, int ACROSS>
+__global__ __launch_bounds__(THREADS) void slope_kernel(SlopeArgs a)
 {
-    __shared__ float lds[8][SLOPE_COLS];
-    const int cx = threadIdx.x % 32, ry = threadIdx.x / 32, c = blockIdx.x * 32 + cx, n = chunk_values(c, a.dim);
+    constexpr int DOWN = THREADS / ACROSS, COLS = ACROSS * CHUNK, PARTS = THREADS / COLS;
+    __shared__ float lds[THREADS * CHUNK];
+    const int cx = threadIdx.x % ACROSS, ry = threadIdx.x / ACROSS, c = blockIdx.x * ACROSS + cx, n = chunk_values(c, a.dim);
     f32x8 s = {};
     if (n > 0)
-        for (int64_t row = (int64_t)blockIdx.y * 8 + ry; row < a.rows; row += SLOPE_ROWS * 8 * (int64_t)gridDim.y) {
+        for (int64_t row = (int64_t)blockIdx.y * DOWN + ry; row < a.rows; row += SLOPE_ROWS * DOWN * (int64_t)gridDim.y) {
             vec<TY, 8> dy[SLOPE_ROWS];
             vec<T, 8> z[SLOPE_ROWS];
             uint64_t q[SLOPE_ROWS];
             uint8_t e[SLOPE_ROWS];
 #pragma unroll
             for (int u = 0; u < SLOPE_ROWS; ++u) {
-                const int64_t at = row + u * 8 * (int64_t)gridDim.y, in = at < a.rows ? at : row;
+                const int64_t at = row + u * DOWN * (int64_t)gridDim.y, in = at < a.rows ? at : row;
                 dy[u] = load_raw<WHOLE>(static_cast<const TY *>(a.dy) + in * a.lddy, c, a.dim);
                 if (a.act == DENSE_ACT_NONE) continue;
                 if (a.q) {
@@ -348,7 +353,7 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
             }
 #pragma unroll
             for (int u = 0; u < SLOPE_ROWS; ++u) {
-                const int64_t at = row + u * 8 * (int64_t)gridDim.y;
+                const int64_t at = row + u * DOWN * (int64_t)gridDim.y;
                 if (at >= a.rows) break;
                 f32x8 d = raw_values<WHOLE>(dy[u], c, a.dim);
                 if (a.act != DENSE_ACT_NONE) {
@@ -367,16 +372,23 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
                 for (int j = 0; j < 8; ++j) s[j] += (WHOLE || j < n) ? d[j] : 0.f;
             }
         }
-    if (!a.partial) return;
+    if (!a.sums) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) lds[ry][cx * CHUNK + j] = s[j];
+    for (int j = 0; j < 8; ++j) lds[threadIdx.x * CHUNK + j] = s[j];       // [row of threads][column]
     __syncthreads();
-    const int col = blockIdx.x * SLOPE_COLS + threadIdx.x, width = (a.dim + CHUNK - 1) / CHUNK * CHUNK;
-    if (col >= width) return;
-    float t = lds[0][threadIdx.x];
+    const int at = threadIdx.x % COLS, part = threadIdx.x / COLS, col = blockIdx.x * COLS + at;
+    float t = lds[part * (DOWN / PARTS) * COLS + at];
 #pragma unroll
-    for (int u = 1; u < 8; ++u) t += lds[u][threadIdx.x];
-    a.partial[(size_t)blockIdx.y * width + col] = t;
+    for (int u = 1; u < DOWN / PARTS; ++u) t += lds[(part * (DOWN / PARTS) + u) * COLS + at];
+    if (PARTS > 1) {
+        __syncthreads();
+        lds[threadIdx.x] = t;
+        __syncthreads();
+        if (part) return;
+#pragma unroll
+        for (int u = 1; u < PARTS; ++u) t += lds[u * COLS + at];
+    }
+    if (col < a.sums_width) a.sums[(size_t)blockIdx.y * a.sums_width + col] = t;
 }
 
 // ---- to 8 bits and back -------------------------------------------------------------------------------
