@@ -32,7 +32,7 @@ int launched()
     return HET_EHIP;
 }
 
-int norm_groups(int64_t rows, const NormShape &h) { return (int)std::min<int64_t>(PARTIALS, cdiv(rows, h.rows)); }
+int norm_groups(int64_t rows, const NormShape &h) { return (int)std::min<int64_t>(h.groups, cdiv(rows, h.rows)); }
 
 void launch_column_sum(const float *partial, int n, int sets, int dim, float *out0, float *out1, hipStream_t st)
 {
@@ -90,26 +90,31 @@ bool linear_sizes(const het_linear_t *l)
            l->rows * std::max(l->in, l->out) <= MOST_VALUES;
 }
 
-// Workgroups down the rows: one where they are few, else enough to fill the chip, a turn of rows for each at least.
+// Threads beside each other in slope_kernel, and workgroups down the rows: one where they are few, else enough to fill the chip, a turn of rows for
+// each at least.
+int slope_across(int32_t out) { return out <= 8 * CHUNK ? 8 : out <= 16 * CHUNK ? 16 : 32; }
 int slope_splits(int64_t rows, int32_t out)
 {
     if (rows <= SLOPE_ALONE_ROWS) return 1;
-    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)PARTIALS, cdiv(rows, SLOPE_THREADS / SLOPE_ACROSS * SLOPE_ROWS), cdiv(2048, cdiv(out, SLOPE_ACROSS * CHUNK))}));
+    const int across = slope_across(out);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)PARTIALS, cdiv(rows, SLOPE_THREADS / across * SLOPE_ROWS), cdiv(2048, cdiv(out, across * CHUNK))}));
 }
 
+template <typename T, typename TY, int THREADS, int ACROSS>
+void launch_slope_of(const SlopeArgs &s, int splits, hipStream_t st)
+{
+    const dim3 grid((uint32_t)cdiv(s.dim, ACROSS * CHUNK), (uint32_t)splits);
+    if (s.dim % CHUNK == 0) slope_kernel<T, TY, true, THREADS, ACROSS><<<grid, THREADS, 0, st>>>(s);
+    else slope_kernel<T, TY, false, THREADS, ACROSS><<<grid, THREADS, 0, st>>>(s);
+}
 template <typename T, typename TY>
 void launch_slope(const SlopeArgs &s, int splits, hipStream_t st)
 {
-    const bool whole = s.dim % CHUNK == 0;
-    if (splits == 1) {
-        const uint32_t grid = (uint32_t)cdiv(s.dim, SLOPE_ALONE_ACROSS * CHUNK);
-        if (whole) slope_kernel<T, TY, true, SLOPE_ALONE_THREADS, SLOPE_ALONE_ACROSS><<<grid, SLOPE_ALONE_THREADS, 0, st>>>(s);
-        else slope_kernel<T, TY, false, SLOPE_ALONE_THREADS, SLOPE_ALONE_ACROSS><<<grid, SLOPE_ALONE_THREADS, 0, st>>>(s);
-        return;
-    }
-    const dim3 grid((uint32_t)cdiv(s.dim, SLOPE_ACROSS * CHUNK), (uint32_t)splits);
-    if (whole) slope_kernel<T, TY, true, SLOPE_THREADS, SLOPE_ACROSS><<<grid, SLOPE_THREADS, 0, st>>>(s);
-    else slope_kernel<T, TY, false, SLOPE_THREADS, SLOPE_ACROSS><<<grid, SLOPE_THREADS, 0, st>>>(s);
+    const int across = slope_across(s.dim);
+    if (splits == 1) launch_slope_of<T, TY, SLOPE_ALONE_THREADS, SLOPE_ALONE_ACROSS>(s, 1, st);
+    else if (across == 8) launch_slope_of<T, TY, SLOPE_THREADS, 8>(s, splits, st);
+    else if (across == 16) launch_slope_of<T, TY, SLOPE_THREADS, 16>(s, splits, st);
+    else launch_slope_of<T, TY, SLOPE_THREADS, 32>(s, splits, st);
 }
 
 // Where a call's scratch lies in its workspace, from 0 on in order, each piece at a multiple of 16 bytes.

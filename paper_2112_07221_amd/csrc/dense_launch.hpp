@@ -25,10 +25,10 @@ void launch_lay(const void *p, int64_t ld, int64_t rows, int width, void *to, in
 // Fills in the sizes of `a` and enqueues the product.
 void launch_product(ProductArgs a, const ProductPlan &p, int type, bool a_k, bool b_k, hipStream_t st);
 
-// How layer norm's rows lie: RowShape, rows a workgroup holds at a time, chunks a lane.
+// How layer norm's rows lie: RowShape, rows a workgroup holds at a time, chunks a lane, the backward pass' workgroups at most.
 struct NormShape {
     RowShape s;
-    int rows, nv;
+    int rows, nv, groups;
     bool block;
 };
 

@@ -30,7 +30,7 @@ NormShape norm_shape(int dim)
     h.s.pitch = (dim + PACK_BLOCK - 1) / PACK_BLOCK * PACK_BLOCK;
     h.block = dim > ROW_WIDE;
     if (h.block) {
-        h.s.lanes = chunks <= 256 ? 256 : chunks <= 512 * 4 ? 512 : 1024;
+        h.s.lanes = chunks <= 128 ? 128 : chunks <= 256 ? 256 : chunks <= 512 * 4 ? 512 : 1024;
         h.rows = 1;
     } else {
         h.s.lanes = 4;
@@ -39,6 +39,9 @@ NormShape norm_shape(int dim)
     }
     const int n = (chunks + h.s.lanes - 1) / h.s.lanes;
     h.nv = n <= 1 ? 1 : n <= 2 ? 2 : 4;
+    // two workgroups of 256 or 512 threads a compute unit, four of 128, and one where a lane has several chunks (their registers leave no more room): backward
+    // of 20000 x 1000 53 us with 512 workgroups of 256 threads, 39 with 1024 of 128; 16384 x 4096 107 with 512, 134 with 256; 8192 x 8192 119 and 109
+    h.groups = h.block && h.s.lanes == 128 ? 2 * (int)PARTIALS : h.nv > 1 ? (int)PARTIALS / 2 : (int)PARTIALS;
     return h;
 }
 #endif

@@ -10,7 +10,7 @@ constexpr int ROW_THREADS = 256;
 constexpr int ROW_WAVES = ROW_THREADS / 64;
 constexpr int ROW_WIDE = 64 * CHUNK;               // widest row that a wave holds, a chunk a lane
 constexpr int ROW_WIDEST = 1024 * CHUNK * 4;       // and a workgroup
-constexpr uint32_t PARTIALS = 512;                 // workgroups that leave partial column sums
+constexpr uint32_t PARTIALS = 512;                 // workgroups that leave partial column sums, about
 
 // How a row lies over lanes.  Rows of up to ROW_WIDE values belong to `lanes` (a power of two, at least a block's four) consecutive lanes of
 // a wave, wider ones to a whole workgroup; lane l holds the chunks l, l + lanes, ...
@@ -102,9 +102,11 @@ __global__ __launch_bounds__(MOST) void norm_kernel(NormArgs a)
     s = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int n = chunk_values(gl + i * lanes, dim);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) { v[i][j] = (WHOLE ? n > 0 : j < n) ? v[i][j] - mean : 0.f; s += v[i][j] * v[i][j]; }
+        for (int j = 0; j < 8; ++j) v[i][j] -= mean;
+        v[i] = chunk_only<WHOLE>(v[i], gl + i * lanes, dim);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += v[i][j] * v[i][j];
     }
     const float rstd = 1.f / sqrtf(sum.one(s) / (float)dim + a.eps);
     if (gl == 0) {
@@ -118,7 +120,7 @@ __global__ __launch_bounds__(MOST) void norm_kernel(NormArgs a)
         f32x8 h;
 #pragma unroll
         for (int j = 0; j < 8; ++j) h[j] = v[i][j] * rstd;
-        if (a.q && c * CHUNK < a.s.pitch) pack_chunk(a.q + row * a.s.pitch, a.e + row * (a.s.pitch / PACK_BLOCK), c, h);
+        if (a.q && c * CHUNK < a.s.pitch) pack_chunk(a.q + row * a.s.pitch, a.e + row * (a.s.pitch / PACK_BLOCK), c, chunk_own<WHOLE>(h, c, dim));
         if (n <= 0) continue;
         const f32x8 g = a.gamma ? load_row<WHOLE>(a.gamma, c, dim) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
         const f32x8 b = a.beta ? load_row<WHOLE>(a.beta, c, dim) : f32x8{};
@@ -164,9 +166,8 @@ struct NormRow {
             const int c = gl + i * lanes;
             dy[i] = load_raw<WHOLE>(static_cast<const TY *>(a.dy) + row * a.lddy, c, dim);
             if (KEPT) {
-                const int in = c * CHUNK < a.s.pitch ? c : 0;
-                __builtin_memcpy(&q[i], a.q + row * a.s.pitch + in * CHUNK, 8);
-                e[i] = a.e[row * (a.s.pitch / PACK_BLOCK) + (in >> 2)];
+                __builtin_memcpy(&q[i], a.q + row * a.s.pitch + chunk_from(c, dim), 8);
+                e[i] = a.e[row * (a.s.pitch / PACK_BLOCK) + (c * CHUNK < dim ? c >> 2 : 0)];
             } else {
                 x[i] = load_raw<WHOLE>(static_cast<const TX *>(a.x) + row * a.ldx, c, dim);
             }
@@ -202,13 +203,18 @@ __global__ __launch_bounds__(MOST) void norm_back_kernel(NormBackArgs a)
         float s1 = 0.f, s2 = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int c = gl + i * lanes, n = chunk_values(c, dim);
+            const int c = gl + i * lanes;
             d[i] = raw_values<WHOLE>(now.dy[i], c, dim);
-            h[i] = KEPT ? unpack_chunk(now.q[i], now.e[i]) : raw_values<WHOLE>(now.x[i], c, dim);
+            if (KEPT) {
+                h[i] = unpack_chunk(now.q[i], now.e[i]);
+            } else {
+                h[i] = __builtin_convertvector(now.x[i], f32x8);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) h[i][j] = (h[i][j] - now.mean) * now.rstd;
+            }
+            h[i] = chunk_only<WHOLE>(h[i], c, dim);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                if (!KEPT) h[i][j] = (h[i][j] - now.mean) * now.rstd;
-                if (WHOLE ? n <= 0 : j >= n) h[i][j] = 0.f;
                 dg[i][j] += d[i][j] * h[i][j];
                 db[i][j] += d[i][j];
                 d[i][j] *= gamma[i][j];
@@ -240,8 +246,8 @@ __global__ __launch_bounds__(MOST) void norm_back_kernel(NormBackArgs a)
         for (int i = 0; i < NV; ++i) {
             const int c = gl + i * lanes;
             if (c * CHUNK >= width) continue;
-            store_chunk(out + c * CHUNK, dg[i]);
-            store_chunk(out + width + c * CHUNK, db[i]);
+            store_chunk(out + c * CHUNK, chunk_own<WHOLE>(dg[i], c, dim));
+            store_chunk(out + width + c * CHUNK, chunk_own<WHOLE>(db[i], c, dim));
         }
         return;
     }
@@ -255,7 +261,7 @@ __global__ __launch_bounds__(MOST) void norm_back_kernel(NormBackArgs a)
         if ((int)threadIdx.x / 64 == w && mine) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const f32x8 &s = u < 2 ? dg[0] : db[0];
+                const f32x8 s = chunk_own<WHOLE>(u < 2 ? dg[0] : db[0], gl, dim);
                 f32x4 v = {s[4 * (u % 2)], s[4 * (u % 2) + 1], s[4 * (u % 2) + 2], s[4 * (u % 2) + 3]};
                 if (w) for (int j = 0; j < 4; ++j) v[j] += at[u][j];
                 at[u] = v;
@@ -319,10 +325,10 @@ struct SlopeArgs {
     int dim, pitch, act, sums_width;
 };
 
-// Many rows: 32 threads beside each other and 8 below, partial sums of many workgroups.  Few rows: one workgroup goes down all of them, 8 threads
-// beside each other and 128 below, and ends the sums itself: no second launch (100 x 4096: 4.7 us; 512 x 512 9.1 and 1001 x 250 21.2, bound by the
-// slope's arithmetic on so few compute units, where workgroups down the rows and the second launch take 5.9 + 3.0).
-constexpr int SLOPE_ACROSS = 32, SLOPE_THREADS = 256, SLOPE_ALONE_ACROSS = 8, SLOPE_ALONE_THREADS = 1024;
+// Many rows: 32 threads beside each other and 8 below (8 and 32 where the layer is narrow: 100000 x 64 30.7 -> 12.9 us), partial sums of many workgroups.  Few rows: one workgroup goes
+// down all of them, 8 threads beside each other and 128 below, and ends the sums itself: no second launch (100 x 4096: 4.7 us; 512 x 512 9.1 and
+// 1001 x 250 21.2, bound by the slope's arithmetic on so few compute units, where workgroups down the rows and the second launch take 5.9 + 3.0).
+constexpr int SLOPE_THREADS = 256, SLOPE_ALONE_ACROSS = 8, SLOPE_ALONE_THREADS = 1024;
 constexpr int SLOPE_ROWS = 2;              // rows a thread has in flight
 constexpr int64_t SLOPE_ALONE_ROWS = 256;  // one turn of them
 
@@ -345,7 +351,7 @@ __global__ __launch_bounds__(THREADS) void slope_kernel(SlopeArgs a)
                 dy[u] = load_raw<WHOLE>(static_cast<const TY *>(a.dy) + in * a.lddy, c, a.dim);
                 if (a.act == DENSE_ACT_NONE) continue;
                 if (a.q) {
-                    __builtin_memcpy(&q[u], a.q + in * a.pitch + c * CHUNK, 8);
+                    __builtin_memcpy(&q[u], a.q + in * a.pitch + chunk_from(c, a.dim), 8);
                     e[u] = a.e[in * (a.pitch / PACK_BLOCK) + (c >> 2)];
                 } else {
                     z[u] = load_raw<WHOLE>(static_cast<const T *>(a.z) + in * a.ldz, c, a.dim);
@@ -357,22 +363,19 @@ __global__ __launch_bounds__(THREADS) void slope_kernel(SlopeArgs a)
                 if (at >= a.rows) break;
                 f32x8 d = raw_values<WHOLE>(dy[u], c, a.dim);
                 if (a.act != DENSE_ACT_NONE) {
-                    const f32x8 slope = act_chunk<true>(a.act, a.q ? unpack_chunk(q[u], e[u]) : raw_values<WHOLE>(z[u], c, a.dim));
+                    const f32x8 slope = act_chunk<true>(a.act, a.q ? unpack_chunk(q[u], e[u]) : __builtin_convertvector(z[u], f32x8));
 #pragma unroll
                     for (int j = 0; j < 8; ++j) d[j] *= slope[j];
+                    d = chunk_only<WHOLE>(d, c, a.dim);
                 }
                 if (a.dz) store_row<WHOLE>(static_cast<T *>(a.dz) + at * a.lddz, c, a.dim, d);
-                if (a.laid) {
-                    f32x8 whole = d;
+                if (a.laid) store_some(static_cast<T *>(a.laid) + at * a.laid_pitch + c * CHUNK, chunk_own<WHOLE>(d, c, a.dim), (int)a.laid_pitch - c * CHUNK);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) whole[j] = (WHOLE || j < n) ? d[j] : 0.f;
-                    store_row<WHOLE>(static_cast<T *>(a.laid) + at * a.laid_pitch, c, (int)a.laid_pitch, whole);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) s[j] += (WHOLE || j < n) ? d[j] : 0.f;
+                for (int j = 0; j < 8; ++j) s[j] += d[j];
             }
         }
     if (!a.sums) return;
+    s = chunk_own<WHOLE>(s, c, a.dim);
 #pragma unroll
     for (int j = 0; j < 8; ++j) lds[threadIdx.x * CHUNK + j] = s[j];       // [row of threads][column]
     __syncthreads();

@@ -81,33 +81,49 @@ __device__ __forceinline__ void store_some(T *p, f32x8 f, int n)
     for (int j = 0; j < CHUNK - 1; ++j) if (j < n) p[j] = (T)f[j];
 }
 
-// Chunk c of a row of `dim` values, zero behind its end, without a branch that lanes take differently, so that the loads of all chunks are
-// under way together.  WHOLE: rows are whole chunks.  Otherwise a lane that would cross the end loads the row's last eight values and
-// shifts them.
+// Chunk c of a row of `dim` values, loaded without a branch that lanes take differently, so that the loads of all chunks are under way together.
+// WHOLE: rows are whole chunks; a chunk behind the end is zero.  Otherwise the chunk that would cross the end is the row's last eight values, of which the
+// first chunk_skip are the chunk before's: they read as zero and are not written.  (Value j of a chunk is column chunk_from + j for all
+// that is loaded, whatever its type, so nothing is shifted: 30000 x 300 forward 23 -> 16, backward 38 -> 30 us.)  A row of less than a chunk is its first chunk's first values.
+__device__ __forceinline__ int chunk_from(int c, int dim)
+{
+    const int last = dim < CHUNK ? 0 : dim - CHUNK;
+    return min(c * CHUNK, last);
+}
+__device__ __forceinline__ int chunk_skip(int c, int dim) { return c * CHUNK - chunk_from(c, dim); }
+// Whether value j of chunk c is one of its own.
+template <bool WHOLE>
+__device__ __forceinline__ bool chunk_has(int c, int j, int dim)
+{
+    if (WHOLE) return c * CHUNK < dim;
+    return dim < CHUNK ? c == 0 && j < dim : j >= chunk_skip(c, dim);
+}
+
+template <bool WHOLE>
+__device__ __forceinline__ f32x8 chunk_only(f32x8 f, int c, int dim)       // zero for the others
+{
+    if (WHOLE) return c * CHUNK < dim ? f : f32x8{};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) f[j] = chunk_has<WHOLE>(c, j, dim) ? f[j] : 0.f;
+    return f;
+}
+
 template <bool WHOLE, typename T>
 __device__ __forceinline__ vec<T, 8> load_raw(const T *row, int c, int dim)
 {
     vec<T, 8> v = {};
-    const int from = c * CHUNK, last = dim - CHUNK;
-    if (!WHOLE && dim < CHUNK) {                         // the whole row is less than a chunk
+    if (!WHOLE && dim < CHUNK) {
 #pragma unroll
-        for (int j = 0; j < CHUNK - 1; ++j) if (from + j < dim) v[j] = row[j];
+        for (int j = 0; j < CHUNK - 1; ++j) if (j < dim) v[j] = row[j];
         return v;
     }
-    __builtin_memcpy(&v, row + (from < last ? from : last), sizeof(v));
+    __builtin_memcpy(&v, row + chunk_from(c, dim), sizeof(v));
     return v;
 }
 template <bool WHOLE, typename T>
 __device__ __forceinline__ f32x8 raw_values(vec<T, 8> v, int c, int dim)
 {
-    f32x8 f = __builtin_convertvector(v, f32x8);
-    const int over = c * CHUNK - (dim - CHUNK);          // values to shift out
-    if (!WHOLE && dim >= CHUNK)
-#pragma unroll
-        for (int by = 4; by >= 1; by /= 2)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = over > 0 && (over & by) ? (j + by < 8 ? f[j + by] : 0.f) : f[j];
-    return over >= CHUNK ? f32x8{} : f;
+    return chunk_only<WHOLE>(__builtin_convertvector(v, f32x8), c, dim);
 }
 template <bool WHOLE, typename T>
 __device__ __forceinline__ f32x8 load_row(const T *row, int c, int dim) { return raw_values<WHOLE>(load_raw<WHOLE>(row, c, dim), c, dim); }
@@ -115,11 +131,28 @@ template <bool WHOLE, bool PAST = false, typename T>
 __device__ __forceinline__ void store_row(T *row, int c, int dim, f32x8 f)
 {
     const int n = dim - c * CHUNK;
-    if constexpr (PAST && sizeof(T) == 2) {
-        if (WHOLE ? n > 0 : n >= CHUNK) { store_past(row + c * CHUNK, __builtin_convertvector(f, vec<T, 8>)); return; }
+    if (WHOLE ? n > 0 : n >= CHUNK) {
+        if constexpr (PAST && sizeof(T) == 2) store_past(row + c * CHUNK, __builtin_convertvector(f, vec<T, 8>));
+        else store_chunk(row + c * CHUNK, f);
+        return;
     }
-    if (WHOLE ? n > 0 : n >= CHUNK) store_chunk(row + c * CHUNK, f);
-    else if (!WHOLE && n > 0) store_some(row + c * CHUNK, f, n);
+    if (WHOLE || n <= 0) return;
+    T *at = row + chunk_from(c, dim);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) if (chunk_has<WHOLE>(c, j, dim)) at[j] = (T)f[j];
+}
+// The chunk's own values from its first place on, zero behind them.
+template <bool WHOLE>
+__device__ __forceinline__ f32x8 chunk_own(f32x8 f, int c, int dim)
+{
+    if (WHOLE || dim < CHUNK) return f;
+    const int over = chunk_skip(c, dim);
+    if (over >= CHUNK) return f32x8{};
+#pragma unroll
+    for (int by = 4; by >= 1; by /= 2)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = over & by ? (j + by < 8 ? f[j + by] : 0.f) : f[j];
+    return f;
 }
 
 // ---- activations --------------------------------------------------------------------------------------
