@@ -108,12 +108,13 @@ def test_calls_without_rows_have_nothing_to_do():
 
 def test_a_workspace_of_the_size_that_is_named_is_needed():
     lib = dense.load()
-    for rows, inp, out, dtype in ((300, 4096, 128, torch.bfloat16), (1, 5000, 9, torch.float32), (70, 9000, 40, torch.float16)):
+    for rows, inp, out, dtype in ((300, 4096, 128, torch.bfloat16), (257, 5000, 9, torch.float32), (700, 9000, 40, torch.float16)):
         need = dense.linear_workspace(rows, inp, out, dtype, backward=True)
         assert need > 0
         l = linear_args(rows=rows, inp=inp, out=out, type=dense.load() and dense._types[dtype], y_type=dense._types[dtype], ldx=inp, ldw=inp, lddx=inp, lddw=inp, lddy=out,
                         lddz=out, ldy=out, workspace_bytes=need - 1)
         assert lib.het_linear_backward(l, None) == HET_EINVAL
+    assert dense.linear_workspace(1, 5000, 9, torch.float32, backward=True) == 0           # few rows' sums are ended where they are formed
     assert dense.linear_workspace(-1, 8, 8, torch.float32) == HET_EINVAL
     assert dense.layer_norm_workspace(4, 0) == HET_EINVAL
 
