@@ -13,7 +13,7 @@ namespace {
 
 constexpr int64_t MOST_ROWS = (1ll << 31) - 1;
 constexpr int32_t MOST_DIM = 1 << 20;
-constexpr int64_t MOST_VALUES = 1ll << 40;          // of one matrix (terabytes): launches of a chunk a thread stay within a grid
+constexpr int64_t MOST_VALUES = 1ll << 40;          // of one matrix (terabytes)
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t align16(int64_t a) { return (a + 15) / 16 * 16; }
@@ -42,21 +42,20 @@ void launch_column_sum(const float *partial, int n, int sets, int dim, float *ou
     column_sum_kernel<<<(uint32_t)cdiv((int64_t)sets * s.width, 16), COLUMN_THREADS, 0, st>>>(s);
 }
 
-// f(tag of x's type, tag of y's type); false: no such pair.
+// f(tag of x's type, tag of y's type) of a known pair.
 template <typename T> struct Tag { using type = T; };
 template <typename F>
-bool with_types(int32_t x, int32_t y, F &&f)
+void with_types(int32_t x, int32_t y, F &&f)
 {
     if (x == HET_F32) {
         if (y == HET_F32) f(Tag<float>(), Tag<float>());
         else if (y == HET_BF16) f(Tag<float>(), Tag<bf16>());
         else f(Tag<float>(), Tag<f16>());
-        return true;
+    } else if (x == HET_BF16) {
+        f(Tag<bf16>(), Tag<bf16>());
+    } else {
+        f(Tag<f16>(), Tag<f16>());
     }
-    if (x != y) return false;
-    if (x == HET_BF16) f(Tag<bf16>(), Tag<bf16>());
-    else f(Tag<f16>(), Tag<f16>());
-    return true;
 }
 template <typename F>
 void with_type(int32_t t, F &&f)
@@ -65,10 +64,16 @@ void with_type(int32_t t, F &&f)
     else if (t == HET_BF16) f(Tag<bf16>());
     else f(Tag<f16>());
 }
-void launch_expand(const ExpandArgs &a, int32_t type, hipStream_t st)
+void launch_expand(const ExpandArgs &all, int32_t type, hipStream_t st)
 {
-    const uint32_t blocks = (uint32_t)cdiv(a.rows * cdiv(a.dim, CHUNK), 256);
-    with_type(type, [&](auto t) { expand_kernel<typename decltype(t)::type><<<blocks, 256, 0, st>>>(a); });
+    const int64_t threads = cdiv(all.dim, CHUNK);
+    in_launches(all.rows, threads, [&](int64_t first, int64_t rows) {
+        ExpandArgs a = all;
+        a.q = moved(a.q, first * a.pitch, 1); a.e = moved(a.e, first * (a.pitch / PACK_BLOCK), 1);
+        a.y = moved(a.y, first * a.ldy, size_of(type));
+        a.rows = rows;
+        with_type(type, [&](auto t) { expand_kernel<typename decltype(t)::type><<<(uint32_t)cdiv(rows * threads, 256), 256, 0, st>>>(a); });
+    });
 }
 
 // An operand laid out at `to`, which it then is.
@@ -224,10 +229,12 @@ int het_pack(const void *x, int32_t type, int64_t ldx, int8_t *q, uint8_t *e, in
 {
     if (!pack_sizes(rows, dim) || !known_type(type) || ldx < dim) return HET_EINVAL;
     if (rows == 0) return HET_OK;
-    const int64_t blocks = cdiv(rows * (pitch_of(dim) / CHUNK), 256);
     if (!x || !q || !e || !aligned16(q)) return HET_EINVAL;
-    PackArgs a{x, q, e, ldx, rows, dim, pitch_of(dim)};
-    with_type(type, [&](auto t) { pack_kernel<typename decltype(t)::type><<<(uint32_t)blocks, 256, 0, static_cast<hipStream_t>(hip_stream)>>>(a); });
+    const int pitch = pitch_of(dim), threads = pitch / CHUNK;
+    in_launches(rows, threads, [&](int64_t first, int64_t some) {
+        const PackArgs a{moved(x, first * ldx, size_of(type)), q + first * pitch, e + first * (pitch / PACK_BLOCK), ldx, some, dim, pitch};
+        with_type(type, [&](auto t) { pack_kernel<typename decltype(t)::type><<<(uint32_t)cdiv(some * threads, 256), 256, 0, static_cast<hipStream_t>(hip_stream)>>>(a); });
+    });
     return launched();
 }
 

@@ -1,9 +1,26 @@
 // Which kernel a call takes, and its launch (dense_product.hip, dense_norm.hip).
 #pragma once
+#include <algorithm>
+
 #include "dense_product.hpp"
 #include "dense_rows.hpp"
 
 namespace het {
+
+// A launch's threads are counted in 32 bits.  Rows of `threads` threads each go in launches of at most 2^31 (and, but for the last, of a
+// multiple of 256 rows, so that no workgroup lies in two): f(first row, rows).
+template <typename F>
+void in_launches(int64_t rows, int64_t threads, F &&f)
+{
+    const int64_t most = std::max<int64_t>((1ll << 31) / threads / 256 * 256, 256);
+    for (int64_t first = 0; first < rows; first += most) f(first, std::min(most, rows - first));
+}
+
+// `p` moved on by a number of values of `size` bytes; null stays null.
+template <typename P> P *moved(P *p, int64_t values, int64_t size)
+{
+    return p ? reinterpret_cast<P *>(reinterpret_cast<uintptr_t>(p) + (uintptr_t)(values * size)) : p;
+}
 
 struct ProductPlan {
     bool ok;                    // the grid fits

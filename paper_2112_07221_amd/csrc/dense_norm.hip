@@ -47,7 +47,7 @@ NormShape norm_shape(int dim)
 #endif
 
 template <bool WHOLE>
-static void norm_of(const NormArgs &a, const NormShape &h, hipStream_t st)
+static void norm_part_of(const NormArgs &a, const NormShape &h, hipStream_t st)
 {
     const uint32_t grid = (uint32_t)((a.rows + h.rows - 1) / h.rows);
     if (!h.block) norm_kernel<X, Y, 1, ROW_THREADS, WHOLE><<<grid, ROW_THREADS, 0, st>>>(a);
@@ -55,6 +55,19 @@ static void norm_of(const NormArgs &a, const NormShape &h, hipStream_t st)
     else if (h.nv == 2) norm_kernel<X, Y, 2, 512, WHOLE><<<grid, h.s.lanes, 0, st>>>(a);
     else if (h.s.lanes == 512) norm_kernel<X, Y, 4, 512, WHOLE><<<grid, h.s.lanes, 0, st>>>(a);
     else norm_kernel<X, Y, 4, 1024, WHOLE><<<grid, h.s.lanes, 0, st>>>(a);
+}
+
+template <bool WHOLE>
+static void norm_of(const NormArgs &all, const NormShape &h, hipStream_t st)
+{
+    in_launches(all.rows, h.s.lanes, [&](int64_t first, int64_t rows) {
+        NormArgs a = all;
+        a.x = moved(a.x, first * a.ldx, sizeof(X)); a.y = moved(a.y, first * a.ldy, sizeof(Y));
+        a.mean = moved(a.mean, first, 4); a.rstd = moved(a.rstd, first, 4);
+        a.q = moved(a.q, first * h.s.pitch, 1); a.e = moved(a.e, first * (h.s.pitch / PACK_BLOCK), 1);
+        a.rows = rows;
+        norm_part_of<WHOLE>(a, h, st);
+    });
 }
 
 template <bool KEPT, bool WHOLE>

@@ -1,8 +1,6 @@
 // Launches of the matrix products; compiled in one part for each type (HET_PART: HET_F32, HET_BF16, HET_F16), the first with the plan.
 #include "../../include/het_dense.h"
 
-#include <algorithm>
-
 #include "dense_launch.hpp"
 
 #define HET_PRODUCT_PARTS 3
@@ -117,7 +115,9 @@ ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bo
     }
     p.k_split = (int)((steps + p.splits - 1) / p.splits * step);
     p.splits = (int)std::max<int64_t>(1, (k + p.k_split - 1) / std::max(p.k_split, 1));
-    p.ok = ((m + 127) / 128) * ((n + 127) / 128) * p.splits <= INT32_MAX && m * ((n + 31) / 32 * 4) / 256 < INT32_MAX;
+    // (rows of x or dz go in several launches if they have to)
+    const int64_t high = p.small_m ? 16 * p.small_m : p.tile, wide = p.small_m ? 16 * p.small_n : p.tile;
+    p.ok = a_k || (m + high - 1) / high * ((n + wide - 1) / wide) * p.splits * (p.small_m ? 64 * SMALL_WAVES : 2 * p.tile) < (1ll << 32);
     p.partial_bytes = p.splits > 1 ? p.splits * m * (int64_t)((n + 15) / 16 * 16) * 4 : 0;
     return p;
 }
@@ -133,21 +133,36 @@ int64_t laid_pitch(int64_t width, int type) { return type == HET_F32 ? (width + 
 
 void launch_lay(const void *p, int64_t ld, int64_t rows, int width, void *to, int type, hipStream_t st)
 {
-    const int64_t pitch = laid_pitch(width, type), pieces = rows * (pitch / (type == HET_F32 ? 4 : 8));
-    const uint32_t grid = (uint32_t)((pieces + 255) / 256);
-    if (type == HET_F32) lay_kernel<uint32_t><<<grid, 256, 0, st>>>(static_cast<const uint32_t *>(p), ld, rows, width, static_cast<uint32_t *>(to), (int)pitch);
-    else lay_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(p), ld, rows, width, static_cast<uint16_t *>(to), (int)pitch);
+    const int64_t pitch = laid_pitch(width, type), pieces = pitch / (type == HET_F32 ? 4 : 8);
+    in_launches(rows, pieces, [&](int64_t first, int64_t some) {
+        const uint32_t grid = (uint32_t)((some * pieces + 255) / 256);
+        if (type == HET_F32) lay_kernel<uint32_t><<<grid, 256, 0, st>>>(static_cast<const uint32_t *>(p) + first * ld, ld, some, width, static_cast<uint32_t *>(to) + first * pitch, (int)pitch);
+        else lay_kernel<uint16_t><<<grid, 256, 0, st>>>(static_cast<const uint16_t *>(p) + first * ld, ld, some, width, static_cast<uint16_t *>(to) + first * pitch, (int)pitch);
+    });
 }
 
-void launch_product(ProductArgs a, const ProductPlan &p, int type, bool a_k, bool b_k, hipStream_t st)
+void launch_product(ProductArgs all, const ProductPlan &p, int type, bool a_k, bool b_k, hipStream_t st)
 {
-    a.m = p.m; a.n = p.n; a.k = p.k;
-    a.splits = p.splits; a.k_split = p.k_split;
-    const int tile = p.tile, high = p.small_m ? 16 * p.small_m : tile, wide = p.small_m ? 16 * (a.f.q ? 2 : p.small_n) : tile;
-    a.tiles_m = (a.m + high - 1) / high; a.tiles_n = (a.n + wide - 1) / wide;
-    if (type == HET_F32) launch_product_of<float>(a, p, a_k, b_k, st);
-    else if (type == HET_BF16) launch_product_of<bf16>(a, p, a_k, b_k, st);
-    else launch_product_of<f16>(a, p, a_k, b_k, st);
+    all.n = p.n; all.k = p.k;
+    all.splits = p.splits; all.k_split = p.k_split;
+    const int tile = p.tile, high = p.small_m ? 16 * p.small_m : tile, wide = p.small_m ? 16 * (all.f.q ? 2 : p.small_n) : tile;
+    all.tiles_n = (all.n + wide - 1) / wide;
+    const int64_t size = type == HET_F32 ? 4 : 2, y_size = all.f.y_f32 ? 4 : 2, threads = (int64_t)all.tiles_n * all.splits * (p.small_m ? 64 * SMALL_WAVES : 2 * tile) / high;
+    const auto part = [&](int64_t first, int64_t rows) {
+        ProductArgs a = all;
+        a.m = (int)rows;
+        a.tiles_m = (a.m + high - 1) / high;
+        if (first) {
+            a.a = moved(a.a, first * a.lda, size);
+            a.f.y = moved(a.f.y, first * a.f.ldy, y_size); a.f.residual = moved(a.f.residual, first * a.f.ldr, y_size); a.f.z = moved(a.f.z, first * a.f.ldz, size);
+            a.f.q = moved(a.f.q, first * a.f.pitch, 1); a.f.e = moved(a.f.e, first * (a.f.pitch / PACK_BLOCK), 1);
+        }
+        if (type == HET_F32) launch_product_of<float>(a, p, a_k, b_k, st);
+        else if (type == HET_BF16) launch_product_of<bf16>(a, p, a_k, b_k, st);
+        else launch_product_of<f16>(a, p, a_k, b_k, st);
+    };
+    if (a_k) in_launches(p.m, threads, part);         // (A's rows are the product's)
+    else part(0, p.m);
 }
 #endif
 

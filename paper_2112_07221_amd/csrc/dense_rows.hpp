@@ -276,7 +276,7 @@ __global__ __launch_bounds__(MOST) void norm_back_kernel(NormBackArgs a)
 }
 
 // Column sums of partial[n][sets][width]: set s goes to out[s] (null: nobody asks).  16 columns a workgroup, 64 threads for each of them, which
-// take every 64th row, eight of them in flight: 512 rows are one turn.  The threads' sums are added in order.
+// take every 64th row, eight of them in flight: the rows of most calls are one turn.  The threads' sums are added in order.
 struct ColumnSumArgs {
     const float *partial;
     float *out[2];
@@ -325,9 +325,10 @@ struct SlopeArgs {
     int dim, pitch, act, sums_width;
 };
 
-// Many rows: 32 threads beside each other and 8 below (8 and 32 where the layer is narrow: 100000 x 64 30.7 -> 12.9 us), partial sums of many workgroups.  Few rows: one workgroup goes
-// down all of them, 8 threads beside each other and 128 below, and ends the sums itself: no second launch (100 x 4096: 4.7 us; 512 x 512 9.1 and
-// 1001 x 250 21.2, bound by the slope's arithmetic on so few compute units, where workgroups down the rows and the second launch take 5.9 + 3.0).
+// Many rows: 32 threads beside each other and 8 below (8 and 32 where the layer is narrow: 100000 x 64 30.7 -> 12.9 us), partial sums of
+// many workgroups.  Few rows: one workgroup goes down all of them, 8 threads beside each other and 128 below, and ends the sums itself: no
+// second launch (100 x 4096: 4.7 us; 512 x 512 9.1 and 1001 x 250 21.2, bound by the slope's arithmetic on so few compute units, where
+// workgroups down the rows and the second launch take 5.9 + 3.0).
 constexpr int SLOPE_THREADS = 256, SLOPE_ALONE_ACROSS = 8, SLOPE_ALONE_THREADS = 1024;
 constexpr int SLOPE_ROWS = 2;              // rows a thread has in flight
 constexpr int64_t SLOPE_ALONE_ROWS = 256;  // one turn of them

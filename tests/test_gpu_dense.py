@@ -598,6 +598,45 @@ def test_a_layer_of_no_input_rows_beyond_and_offsets_past_32_bits():
     assert torch.equal(dx, dx2) and torch.equal(dw, dw2)
 
 
+def test_more_threads_than_a_launch_holds():
+    """2^30 and some narrow rows: over 2^32 threads at a few for a row.  The rows repeat, and so do the results, bit for bit: a row's are its own."""
+    period, times = 65537, 16385
+    rows = period * times
+    assert rows > 1 << 30
+    g = gen(8)
+
+    def repeats(got, want):
+        return all(bool((part == want).all()) for part in got.view(times, period, -1).split(1024))
+
+    base = torch.randint(-64, 65, (period, 2), generator=g).to(BF16).cuda()         # (whole numbers: products and sums are exact, whichever kernel)
+    x = base.repeat(times, 1)
+    want, y = torch.empty_like(base), torch.empty_like(x)
+    dense.layer_norm(base, None, None, want)
+    dense.layer_norm(x, None, None, y)
+    assert repeats(y, want)
+    w = torch.tensor([[3.0, -5.0]], dtype=BF16, device="cuda")
+    bias = torch.randn(1, generator=g).cuda()
+    want, want_z = (torch.empty(period, 1, dtype=BF16, device="cuda") for _ in range(2))
+    y, z = (torch.empty(rows, 1, dtype=BF16, device="cuda") for _ in range(2))
+    dense.linear(base, w, bias, want, dense.ACT_SILU, None, want_z)
+    dense.linear(x, w, bias, y, dense.ACT_SILU, None, z)
+    assert repeats(y, want) and repeats(z, want_z)
+    dy, want = torch.randn(period, 1, generator=g).to(BF16).cuda(), torch.empty_like(base)
+    all_dy = dy.repeat(times, 1)
+    dense.linear_backward(dy, base, w, None, dense.ACT_NONE, None, want, None)
+    dense.linear_backward(all_dy, x, w, None, dense.ACT_NONE, None, x, None)         # (x is not read: no dw is asked for)
+    assert repeats(x, want)
+    del x, z, all_dy
+    want, got = dense.Packed.empty(period, 1), dense.Packed.empty(rows, 1)
+    dense.pack(dy, want)
+    dense.pack(dy.repeat(times, 1), got)
+    assert repeats(got.q, want.q) and repeats(got.e, want.e)
+    back = torch.empty_like(dy)
+    dense.expand(want, back)
+    dense.expand(got, y)
+    assert repeats(y, back)
+
+
 def test_a_workspace_that_is_too_small_is_refused():
     x, w, y = torch.zeros(1000, 16384, device="cuda"), torch.zeros(300, 16384, device="cuda"), torch.zeros(1000, 300, device="cuda")
     need = dense.linear_workspace(1000, 16384, 300, F32)                # a long sum over few tiles is split
