@@ -5,7 +5,6 @@
 #include <cstdio>
 
 #include "dense_launch.hpp"
-#include "dense_rows.hpp"
 
 using namespace het;
 
@@ -34,12 +33,13 @@ int launched()
 
 int norm_groups(int64_t rows, const NormShape &h) { return (int)std::min<int64_t>(h.groups, cdiv(rows, h.rows)); }
 
-void launch_column_sum(const float *partial, int n, int sets, int dim, float *out0, float *out1, hipStream_t st)
+ColumnSumArgs column_sums(const float *partial, int n, int sets, int dim, float *out0, float *out1)
 {
-    ColumnSumArgs s;
-    s.partial = partial; s.out[0] = out0; s.out[1] = out1;
-    s.n = n; s.sets = sets; s.width = width_of(dim); s.dim = dim;
-    column_sum_kernel<<<(uint32_t)cdiv((int64_t)sets * s.width, 16), COLUMN_THREADS, 0, st>>>(s);
+    return ColumnSumArgs{partial, {out0, out1}, n, sets, width_of(dim), dim};
+}
+void launch_column_sum(const ColumnSumArgs &s, hipStream_t st)
+{
+    column_sum_kernel<<<(uint32_t)cdiv((int64_t)s.sets * s.width, 16), COLUMN_THREADS, 0, st>>>(s);
 }
 
 // f(tag of x's type, tag of y's type) of a known pair.
@@ -221,7 +221,7 @@ int het_layer_norm_backward(const void *dy, int32_t y_type, int64_t lddy, const 
             launch_norm_back<typename decltype(tx)::type, typename decltype(ty)::type>(a, h, groups, st);
         });
     }
-    if (dgamma || dbeta) launch_column_sum(partial, groups, 2, dim, dgamma, dbeta, st);
+    if (dgamma || dbeta) launch_column_sum(column_sums(partial, groups, 2, dim, dgamma, dbeta), st);
     return launched();
 }
 
@@ -301,6 +301,7 @@ int het_linear_backward(const het_linear_t *l, void *hip_stream)
     char *ws = static_cast<char *>(l->workspace);
     const void *dz = dz_is_dy ? l->dy : l->dz, *laid = dz;
     int64_t lddz = dz_is_dy ? l->lddy : l->lddz, ld_laid = lddz;
+    ColumnSumArgs bias{};               // dbias' parts, if they are still to be added up
     if (p.runs_slope) {
         SlopeArgs s{};
         s.dy = l->dy; s.lddy = l->lddy;
@@ -312,32 +313,35 @@ int het_linear_backward(const het_linear_t *l, void *hip_stream)
         s.sums_width = alone ? l->out : width_of(l->out);
         s.rows = l->rows; s.dim = l->out; s.pitch = pitch_of(l->out); s.act = l->act;
         with_types(l->y_type, l->type, [&](auto ty, auto t) { launch_slope<typename decltype(t)::type, typename decltype(ty)::type>(s, p.slope, st); });
-        if (l->dbias && !alone) launch_column_sum(s.sums, p.slope, 1, l->out, l->dbias, nullptr, st);
+        if (l->dbias && !alone) bias = column_sums(s.sums, p.slope, 1, l->out, l->dbias, nullptr);
     } else if (p.lay_dz) {
         lay(laid, ld_laid, l->rows, l->out, ws + p.dz_at, l->type, st);
     }
-    ProductArgs a{};
-    a.partial = reinterpret_cast<float *>(ws + p.partial_at);
-    a.f.y_f32 = l->type == HET_F32;
-    if (l->dx && some) {
-        a.a = p.dx.lay_a ? laid : dz; a.lda = p.dx.lay_a ? ld_laid : lddz;
-        a.b = l->w; a.ldb = l->ldw;
-        if (p.dx.lay_b) lay(a.b, a.ldb, l->out, l->in, ws + p.w_at, l->type, st);
-        a.f.y = l->dx; a.f.ldy = l->lddx;
-        launch_product(a, p.dx, l->type, true, false, st);
+    ProductArgs dx{}, dw{};
+    dx.partial = dw.partial = reinterpret_cast<float *>(ws + p.partial_at);
+    dx.f.y_f32 = dw.f.y_f32 = l->type == HET_F32;
+    const bool wants_dx = l->dx && some;
+    if (wants_dx) {
+        dx.a = p.dx.lay_a ? laid : dz; dx.lda = p.dx.lay_a ? ld_laid : lddz;
+        dx.b = l->w; dx.ldb = l->ldw;
+        if (p.dx.lay_b) lay(dx.b, dx.ldb, l->out, l->in, ws + p.w_at, l->type, st);
+        dx.f.y = l->dx; dx.f.ldy = l->lddx;
     }
     if (l->dw) {
-        a.a = p.dw.lay_a ? laid : dz; a.lda = p.dw.lay_a ? ld_laid : lddz;
-        a.b = l->x; a.ldb = l->ldx;
+        dw.a = p.dw.lay_a ? laid : dz; dw.lda = p.dw.lay_a ? ld_laid : lddz;
+        dw.b = l->x; dw.ldb = l->ldx;
         if (l->xq) {
-            a.b = ws + p.x_at; a.ldb = p.ldx;
+            dw.b = ws + p.x_at; dw.ldb = p.ldx;
             if (some) launch_expand(ExpandArgs{l->xq, l->xe, l->x_gamma, l->x_beta, ws + p.x_at, p.ldx, l->rows, l->in, pitch_of(l->in), l->x_act}, l->type, st);
         } else if (p.dw.lay_b) {
-            lay(a.b, a.ldb, l->rows, l->in, ws + p.x_at, l->type, st);
+            lay(dw.b, dw.ldb, l->rows, l->in, ws + p.x_at, l->type, st);
         }
-        a.f.y = l->dw; a.f.ldy = l->lddw;
-        launch_product(a, p.dw, l->type, false, false, st);
+        dw.f.y = l->dw; dw.f.ldy = l->lddw;
     }
+    if (wants_dx && l->dw && launch_small_back(dw, p.dw, dx, p.dx, bias, l->type, st)) return launched();
+    if (bias.n) launch_column_sum(bias, st);
+    if (wants_dx) launch_product(dx, p.dx, l->type, true, false, st);
+    if (l->dw) launch_product(dw, p.dw, l->type, false, false, st);
     return launched();
 }
 

@@ -3,7 +3,6 @@
 #include <algorithm>
 
 #include "dense_product.hpp"
-#include "dense_rows.hpp"
 
 namespace het {
 
@@ -38,6 +37,10 @@ bool product_lies(const void *p, int64_t ld, int64_t width, int type);
 // Rows of `width` values as product_kernel takes them: values from a row to the next, and their launch.
 int64_t laid_pitch(int64_t width, int type);
 void launch_lay(const void *p, int64_t ld, int64_t rows, int width, void *to, int type, hipStream_t st);
+
+// Both products of a small layer's backward pass and the sums of dbias' parts (bias.n: 0 for none) in one launch; false if they are not for one, and
+// nothing is enqueued.
+bool launch_small_back(ProductArgs dw, const ProductPlan &dw_plan, ProductArgs dx, const ProductPlan &dx_plan, const ColumnSumArgs &bias, int type, hipStream_t st);
 
 // Fills in the sizes of `a` and enqueues the product.
 void launch_product(ProductArgs a, const ProductPlan &p, int type, bool a_k, bool b_k, hipStream_t st);

@@ -9,6 +9,7 @@ static_assert(HET_PARTS == HET_PRODUCT_PARTS, "the build compiles other parts th
 namespace het {
 
 template <typename T> void launch_product_of(const ProductArgs &a, const ProductPlan &p, bool a_k, bool b_k, hipStream_t st);
+template <typename T> void launch_small_back_of(const SmallBackArgs &a, int nw, int nx, uint32_t grid, hipStream_t st);
 
 #if HET_PART == 0
 using PartType = float;
@@ -54,9 +55,24 @@ void launch_product_of(const ProductArgs &a, const ProductPlan &p, bool a_k, boo
     }
 }
 
+template <typename T>
+void launch_small_back_of(const SmallBackArgs &a, int nw, int nx, uint32_t grid, hipStream_t st)
+{
+    if (nw == 1) {
+        if (nx == 1) small_back_kernel<T, 1, 1><<<grid, 64 * SMALL_WAVES, 0, st>>>(a);
+        else small_back_kernel<T, 1, 2><<<grid, 64 * SMALL_WAVES, 0, st>>>(a);
+    } else {
+        if (nx == 1) small_back_kernel<T, 2, 1><<<grid, 64 * SMALL_WAVES, 0, st>>>(a);
+        else small_back_kernel<T, 2, 2><<<grid, 64 * SMALL_WAVES, 0, st>>>(a);
+    }
+}
+
+template void launch_small_back_of<PartType>(const SmallBackArgs &, int, int, uint32_t, hipStream_t);
 template void launch_product_of<PartType>(const ProductArgs &, const ProductPlan &, bool, bool, hipStream_t);
 
 #if HET_PART == 0
+extern template void launch_small_back_of<bf16>(const SmallBackArgs &, int, int, uint32_t, hipStream_t);
+extern template void launch_small_back_of<f16>(const SmallBackArgs &, int, int, uint32_t, hipStream_t);
 extern template void launch_product_of<bf16>(const ProductArgs &, const ProductPlan &, bool, bool, hipStream_t);
 extern template void launch_product_of<f16>(const ProductArgs &, const ProductPlan &, bool, bool, hipStream_t);
 
@@ -163,6 +179,29 @@ void launch_product(ProductArgs all, const ProductPlan &p, int type, bool a_k, b
     };
     if (a_k) in_launches(p.m, threads, part);         // (A's rows are the product's)
     else part(0, p.m);
+}
+
+// Sizes of a product of product_small_kernel's; its workgroups.
+static int64_t small_sizes(ProductArgs &a, const ProductPlan &p)
+{
+    a.m = p.m; a.n = p.n; a.k = p.k;
+    a.splits = p.splits; a.k_split = p.k_split;
+    a.tiles_m = (a.m + 16 * p.small_m - 1) / (16 * p.small_m); a.tiles_n = (a.n + 16 * p.small_n - 1) / (16 * p.small_n);
+    return (int64_t)a.tiles_m * a.tiles_n;
+}
+
+bool launch_small_back(ProductArgs dw, const ProductPlan &dw_plan, ProductArgs dx, const ProductPlan &dx_plan, const ColumnSumArgs &bias, int type, hipStream_t st)
+{
+    if (dw_plan.small_m != 2 || dx_plan.small_m != 2) return false;
+    SmallBackArgs a{dw, dx, bias, 0, 0};
+    const int64_t w = small_sizes(a.dw, dw_plan), x = small_sizes(a.dx, dx_plan), b = bias.n ? (bias.sets * bias.width + 15) / 16 : 0;
+    if ((w + x + b) * 64 * SMALL_WAVES >= 1ll << 31) return false;
+    a.dw_groups = (int)w; a.dx_groups = (int)x;
+    const uint32_t grid = (uint32_t)(w + x + b);
+    if (type == HET_F32) launch_small_back_of<float>(a, dw_plan.small_n, dx_plan.small_n, grid, st);
+    else if (type == HET_BF16) launch_small_back_of<bf16>(a, dw_plan.small_n, dx_plan.small_n, grid, st);
+    else launch_small_back_of<f16>(a, dw_plan.small_n, dx_plan.small_n, grid, st);
+    return true;
 }
 #endif
 

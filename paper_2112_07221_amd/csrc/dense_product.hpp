@@ -4,7 +4,7 @@
 // All are D[m][n] = sum over k of A(m, k) B(n, k).  An operand is read along k (K: its rows are A's or B's, as x and w are in x w^T) or
 // across (its rows are k's, as w is in dz w, and both are in dz^T x); nothing is transposed in memory.
 #pragma once
-#include "dense_types.hpp"
+#include "dense_rows.hpp"
 
 namespace het {
 
@@ -499,15 +499,16 @@ struct Direct {
     }
 };
 
+template <int MT, int NT> struct SmallRoom { float sums[SMALL_WAVES][16 * MT][16 * NT + 4]; };
+
 template <typename T, bool AK, bool BK, int MT, int NT>
-__global__ __launch_bounds__(64 * SMALL_WAVES) void product_small_kernel(ProductArgs a)
+__device__ __forceinline__ void product_small(const ProductArgs &a, int block, float (*lds)[16 * MT][16 * NT + 4])
 {
     using DA = Direct<T, AK>;
     using DB = Direct<T, BK>;
     constexpr int SPAN = 8 * DA::PIECE, AHEAD = MT * NT == 1 ? 4 : 2;
-    __shared__ float lds[SMALL_WAVES][16 * MT][16 * NT + 4];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), r = lane % 16, g = lane / 16;
-    const int row0 = blockIdx.x / a.tiles_n * 16 * MT, col0 = blockIdx.x % a.tiles_n * 16 * NT;
+    const int row0 = block / a.tiles_n * 16 * MT, col0 = block % a.tiles_n * 16 * NT;
     // the chunk this thread ends, and what is added to it, asked for ahead
     const int c = threadIdx.x % (2 * NT), at = threadIdx.x / (2 * NT), row = row0 + at, col = col0 + c * CHUNK, n = a.n - col;
     const bool ends = at < 16 * MT && row < a.m;
@@ -573,6 +574,32 @@ __global__ __launch_bounds__(64 * SMALL_WAVES) void product_small_kernel(Product
     v = plus(v, bias);
     if (NT == 2 && a.f.q) pack_chunk(a.f.q + (int64_t)row * a.f.pitch, a.f.e + (int64_t)row * (a.f.pitch / PACK_BLOCK), col / CHUNK, v);
     finish_value<T>(a.f, row, col, n, v, residual);
+}
+
+template <typename T, bool AK, bool BK, int MT, int NT>
+__global__ __launch_bounds__(64 * SMALL_WAVES) void product_small_kernel(ProductArgs a)
+{
+    __shared__ SmallRoom<MT, NT> lds;
+    product_small<T, AK, BK, MT, NT>(a, blockIdx.x, lds.sums);
+}
+
+// What a small layer's backward pass does once dz is there, in one launch: dw, dx, and the sums of dbias' parts.  None needs another's results, and
+// each alone leaves most of the chip waiting for memory (PAIR_MEASURED).
+struct SmallBackArgs {
+    ProductArgs dw, dx;
+    ColumnSumArgs bias;
+    int dw_groups, dx_groups;           // workgroups of each; those behind them are the sums'
+};
+
+template <typename T, int NW, int NX>
+__global__ __launch_bounds__(64 * SMALL_WAVES) void small_back_kernel(SmallBackArgs a)
+{
+    __shared__ union { SmallRoom<2, NW> dw; SmallRoom<2, NX> dx; float bias[4 * SMALL_WAVES][17]; } lds;
+    int block = blockIdx.x;
+    if (block < a.dw_groups) return product_small<T, false, false, 2, NW>(a.dw, block, lds.dw.sums);
+    block -= a.dw_groups;
+    if (block < a.dx_groups) return product_small<T, true, false, 2, NX>(a.dx, block, lds.dx.sums);
+    column_sum<64 * SMALL_WAVES>(a.bias, block - a.dx_groups, lds.bias);
 }
 
 } // namespace het

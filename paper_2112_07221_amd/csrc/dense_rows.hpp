@@ -275,8 +275,8 @@ __global__ __launch_bounds__(MOST) void norm_back_kernel(NormBackArgs a)
     }
 }
 
-// Column sums of partial[n][sets][width]: set s goes to out[s] (null: nobody asks).  16 columns a workgroup, 64 threads for each of them, which
-// take every 64th row, eight of them in flight: the rows of most calls are one turn.  The threads' sums are added in order.
+// Column sums of partial[n][sets][width]: set s goes to out[s] (null: nobody asks).  16 columns a workgroup, THREADS / 16 threads for
+// each of them, which take every so manieth row, eight of them in flight: with 1024 threads the rows of most calls are one turn.  The threads' sums are added in order.
 struct ColumnSumArgs {
     const float *partial;
     float *out[2];
@@ -285,11 +285,11 @@ struct ColumnSumArgs {
 
 constexpr int COLUMN_THREADS = 1024;
 
-static __global__ __launch_bounds__(COLUMN_THREADS) void column_sum_kernel(ColumnSumArgs a)
+template <int THREADS>
+__device__ __forceinline__ void column_sum(const ColumnSumArgs &a, int block, float (*lds)[17])       // lds: [THREADS / 16]
 {
-    constexpr int DEEP = COLUMN_THREADS / 16;
-    __shared__ float lds[DEEP][17];
-    const int cx = threadIdx.x % 16, ry = threadIdx.x / 16, col = blockIdx.x * 16 + cx, total = a.sets * a.width;
+    constexpr int DEEP = THREADS / 16;
+    const int cx = threadIdx.x % 16, ry = threadIdx.x / 16, col = block * 16 + cx, total = a.sets * a.width;
     const float *p = a.partial + (col < total ? col : 0);
     float s = 0.f;
     for (int r = ry; r < a.n; r += 8 * DEEP) {
@@ -309,6 +309,12 @@ static __global__ __launch_bounds__(COLUMN_THREADS) void column_sum_kernel(Colum
     if (ry || col >= total) return;
     const int set = col / a.width, at = col % a.width;
     if (at < a.dim && a.out[set]) a.out[set][at] = s;
+}
+
+static __global__ __launch_bounds__(COLUMN_THREADS) void column_sum_kernel(ColumnSumArgs a)
+{
+    __shared__ float lds[COLUMN_THREADS / 16][17];
+    column_sum<COLUMN_THREADS>(a, blockIdx.x, lds);
 }
 
 // ---- the slope of the activation and the bias' gradient -------------------------------------------------
