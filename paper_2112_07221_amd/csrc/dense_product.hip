@@ -51,7 +51,8 @@ void launch_product_of(const ProductArgs &a, const ProductPlan &p, bool a_k, boo
     }
     if (a.splits > 1) {
         const int64_t per = (a.n + PACK_BLOCK - 1) / PACK_BLOCK * 4;
-        join_kernel<T><<<(uint32_t)((a.m * per + 255) / 256), 256, 0, st>>>(a);
+        if (a.splits > 8) join_kernel<T, 8><<<(uint32_t)((a.m * per + 31) / 32), 256, 0, st>>>(a);
+        else join_kernel<T, 1><<<(uint32_t)((a.m * per + 255) / 256), 256, 0, st>>>(a);
     }
 }
 
@@ -76,29 +77,30 @@ extern template void launch_small_back_of<f16>(const SmallBackArgs &, int, int, 
 extern template void launch_product_of<bf16>(const ProductArgs &, const ProductPlan &, bool, bool, hipStream_t);
 extern template void launch_product_of<f16>(const ProductArgs &, const ProductPlan &, bool, bool, hipStream_t);
 
-constexpr int64_t CUS = 256;
+constexpr int64_t CUS = 256, MOST_SPLITS = 128;
 
-// Microseconds a product takes with tiles of 256 or 128 and its k's split, by the times measured at 64 .. 8192 rows, columns and k's in bf16 and
+// Microseconds a product takes with tiles of 256 or 128 and its k's split, by the times measured at 16 .. 16384 rows, columns and k's in bf16 and
 // fp32: a tile of 256 has a compute unit to itself, of 128 two share one.  Adding up the splits costs a launch and the sums' way through memory.
 // 4096 x 1664 -> 4096 in bf16: 256 48, 128 54 us; 2048 x 2048 -> 2048: 43 and 27; dw of 16384 x 896 -> 4096: 128 175, split in two 126, 256 split in
-// four 129.  Tiles of 256 x 128 (two waves' 64 x 64 side by side, one workgroup a compute unit) were slower than one of the two everywhere.
-static double tiles_us(int tile, int64_t tiles, int64_t splits, int64_t steps, int64_t m, int64_t n, bool f32)
+// four 129; dw of 100000 x 64 -> 64: split in 32 34 + 10, in 128 13 + 6.  Tiles of 256 x 128 (two waves' 64 x 64 side by side, one workgroup a compute
+// unit) were slower than one of the two everywhere.
+static double tiles_us(int tile, int64_t tiles, int64_t splits, int64_t steps, int64_t m, int64_t n, bool f32, bool b_k)
 {
-    const double s = (double)((steps + splits - 1) / splits);
+    const double s = (double)((steps + splits - 1) / splits), start = b_k ? 4 : 7;
     const int64_t groups = tiles * splits, turns = (groups + CUS - 1) / CUS;
     double us = 0;
     if (tile == 256) us = (double)turns * (10 + (f32 ? 7.3 : 1.5) * s);
-    else us = (double)(turns / 2) * (6 + (f32 ? 4.1 : 0.8) * s) + (double)(turns % 2) * (4 + (f32 ? 2.1 : 0.62) * s);
+    else us = (double)(turns / 2) * (start + 2 + (f32 ? 4.1 : 0.8) * s) + (double)(turns % 2) * (start + (f32 ? 2.1 : 0.62) * s);
     return splits > 1 ? us + 3 + (double)splits * (double)m * (double)n * 1.4e-6 : us;
 }
 
 // ... and with product_small_kernel: its waves' turns through k (a step is a span, two of them at a time), a thousand workgroups at a time, and the
 // operands out of the L2 once for every 32 rows or columns.  1001 x 500 -> 250 in fp16: 7.6 .. 8.4 us a product, tiles 16.6 .. 20.4; 2048 x 1024 ->
-// 1024 in bf16: 30.6, tiles 11.4; a single token 1664 -> 1024: 7.9, tiles 12.7 (each with the launch).
+// 1024 in bf16: 30.6, tiles 11.4; a single token 1664 -> 1024: 7.9, tiles 12.7; dx of 16384 x 16 -> 64: 3.8, tiles 7.3 (each with the launch).
 static double small_us(int64_t steps, int64_t m, int64_t n, int64_t k, bool a_k, bool b_k, bool f32)
 {
     const int64_t high = a_k && b_k && m <= 16 ? 16 : (m + 31) / 32 * 32, wide = (n + 31) / 32 * 32;
-    const double turn = a_k && b_k ? 1.0 : a_k ? 1.5 : 2.0, each = f32 ? 28e-9 : a_k && b_k ? 12e-9 : 20e-9;
+    const double turn = a_k ? 1 : 2, each = f32 ? 28e-9 : a_k && b_k ? 12e-9 : 20e-9;
     return 1 + turn * (double)((steps + 2 * SMALL_WAVES - 1) / (2 * SMALL_WAVES)) + 4.0 / 1024 * (double)high * (double)wide / 1024 +
            each * (double)high * (double)wide * (double)k;
 }
@@ -112,15 +114,18 @@ ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bo
     ProductPlan p{};
     p.lay_a = !lies_a; p.lay_b = !lies_b;
     p.m = (int)m; p.n = (int)n; p.k = (int)k;
-    p.splits = 1;
-    const int64_t step = f32 ? 32 : 64, steps = (k + step - 1) / step;
     double best = 1e30;
+    const int64_t step = f32 ? 32 : 64, steps = (k + step - 1) / step;
     for (int tile = 256; tile >= 128; tile /= 2) {
-        const int64_t tiles = ((m + tile - 1) / tile) * ((n + tile - 1) / tile);
-        for (int64_t splits = 1; splits <= 32 && (splits == 1 || (splits * 4 <= steps && tiles * splits <= 4 * CUS)); ++splits) {
-            const double us = tiles_us(tile, tiles, splits, steps, m, n, f32);
+        const int64_t tiles = std::max<int64_t>(1, ((m + tile - 1) / tile) * ((n + tile - 1) / tile));
+        const int64_t most = std::max<int64_t>(1, std::min({MOST_SPLITS, steps / 4, 4 * CUS / tiles}));
+        const auto of = [&](int64_t splits) {
+            const double us = tiles_us(tile, tiles, splits, steps, m, n, f32, b_k);
             if (us < best) { best = us; p.tile = tile; p.splits = (int)splits; }
-        }
+        };
+        // every number of splits up to 8, then fewer and fewer, and those that fill the compute units' turns
+        for (int64_t splits = 1; splits <= most; splits += splits < 8 ? 1 : splits / 4) of(splits);
+        for (int64_t turns = 1; turns <= 4 && most > 8; turns *= 2) of(std::max<int64_t>(1, std::min(most, turns * CUS / tiles)));
     }
     best += (p.lay_a ? lay_us(m, k, f32) : 0) + (p.lay_b ? lay_us(n, k, f32) : 0);
     if (small_us(steps, m, n, k, a_k, b_k, f32) < best) {

@@ -275,8 +275,8 @@ __global__ __launch_bounds__(MOST) void norm_back_kernel(NormBackArgs a)
     }
 }
 
-// Column sums of partial[n][sets][width]: set s goes to out[s] (null: nobody asks).  16 columns a workgroup, THREADS / 16 threads for
-// each of them, which take every so manieth row, eight of them in flight: with 1024 threads the rows of most calls are one turn.  The threads' sums are added in order.
+// Column sums of partial[n][sets][width]: set s goes to out[s] (null: nobody asks).  16 columns a workgroup, for each of them 64 sums of
+// every 64th row, eight rows in flight, which are added in order: the same bits whatever the number of threads.
 struct ColumnSumArgs {
     const float *partial;
     float *out[2];
@@ -285,21 +285,27 @@ struct ColumnSumArgs {
 
 constexpr int COLUMN_THREADS = 1024;
 
+constexpr int COLUMN_DEEP = 64;
+
 template <int THREADS>
-__device__ __forceinline__ void column_sum(const ColumnSumArgs &a, int block, float (*lds)[17])       // lds: [THREADS / 16]
+__device__ __forceinline__ void column_sum(const ColumnSumArgs &a, int block, float (*lds)[17])       // lds: [COLUMN_DEEP]
 {
-    constexpr int DEEP = THREADS / 16;
+    constexpr int DEEP = COLUMN_DEEP;
     const int cx = threadIdx.x % 16, ry = threadIdx.x / 16, col = block * 16 + cx, total = a.sets * a.width;
     const float *p = a.partial + (col < total ? col : 0);
     float s = 0.f;
-    for (int r = ry; r < a.n; r += 8 * DEEP) {
-        float v[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) v[u] = p[(size_t)(r + u * DEEP < a.n ? r + u * DEEP : r) * total];
+    for (int first = DEEP - THREADS / 16; first >= 0; first -= THREADS / 16) {             // (the thread's own row of sums last: it goes on with it)
+        s = 0.f;
+        for (int r = ry + first; r < a.n; r += 8 * DEEP) {
+            float v[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) s += r + u * DEEP < a.n ? v[u] : 0.f;
+            for (int u = 0; u < 8; ++u) v[u] = p[(size_t)(r + u * DEEP < a.n ? r + u * DEEP : r) * total];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) s += r + u * DEEP < a.n ? v[u] : 0.f;
+        }
+        lds[ry + first][cx] = s;
     }
-    lds[ry][cx] = s;
     __syncthreads();
     if (ry >= 4) return;                                  // four threads a column, then one
 #pragma unroll
@@ -313,7 +319,7 @@ __device__ __forceinline__ void column_sum(const ColumnSumArgs &a, int block, fl
 
 static __global__ __launch_bounds__(COLUMN_THREADS) void column_sum_kernel(ColumnSumArgs a)
 {
-    __shared__ float lds[COLUMN_THREADS / 16][17];
+    __shared__ float lds[COLUMN_DEEP][17];
     column_sum<COLUMN_THREADS>(a, blockIdx.x, lds);
 }
 
