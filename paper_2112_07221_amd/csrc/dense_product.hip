@@ -8,6 +8,8 @@ static_assert(HET_PARTS == HET_PRODUCT_PARTS, "the build compiles other parts th
 
 namespace het {
 
+constexpr int64_t CUS = 256, MOST_SPLITS = 128, DEEP_STEPS = 4;
+
 template <typename T> void launch_product_of(const ProductArgs &a, const ProductPlan &p, bool a_k, bool b_k, hipStream_t st);
 template <typename T> void launch_small_back_of(const SmallBackArgs &a, int nw, int nx, uint32_t grid, hipStream_t st);
 
@@ -40,20 +42,32 @@ void launch_product_of(const ProductArgs &a, const ProductPlan &p, bool a_k, boo
         return;
     }
     const uint32_t grid = (uint32_t)(a.tiles_m * a.tiles_n * a.splits);
-    if (p.tile == 256) {
-        if (a_k && b_k) product_kernel<T, true, true, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
-        else if (a_k) product_kernel<T, true, false, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
-        else product_kernel<T, false, false, 256, 256, 2, 4><<<grid, 512, 0, st>>>(a);
-    } else {
-        if (a_k && b_k) product_kernel<T, true, true, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
-        else if (a_k) product_kernel<T, true, false, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
-        else product_kernel<T, false, false, 128, 128, 2, 2><<<grid, 256, 0, st>>>(a);
-    }
-    if (a.splits > 1) {
+    const auto joined = [&] {
+        if (a.splits == 1) return;
         const int64_t per = (a.n + PACK_BLOCK - 1) / PACK_BLOCK * 4;
         if (a.splits > 8) join_kernel<T, 8><<<(uint32_t)((a.m * per + 31) / 32), 256, 0, st>>>(a);
         else join_kernel<T, 1><<<(uint32_t)((a.m * per + 255) / 256), 256, 0, st>>>(a);
+    };
+    if (p.tile == 256) {
+        if (a_k && b_k) product_kernel<T, true, true, 256, 256, 2, 4, 2><<<grid, 512, 0, st>>>(a);
+        else if (a_k) product_kernel<T, true, false, 256, 256, 2, 4, 2><<<grid, 512, 0, st>>>(a);
+        else product_kernel<T, false, false, 256, 256, 2, 4, 2><<<grid, 512, 0, st>>>(a);
+        return joined();
     }
+    // A tile alone on its compute unit waits for its copies unless they are further ahead, a pair for each other's; in fp32 the products take longer than
+    // the copies (2048 x 2048 -> 2048 in bf16 28.0 us with two buffers, 20.8 with four; 1024 x 4096 -> 4096 46.3 and 35.3; fp32 62.5 and 66.3).  It goes in turns of four
+    // steps: fewer are not worth it.
+    if constexpr (sizeof(T) == 2)
+        if (grid <= CUS && a.k_split >= DEEP_STEPS * 64) {
+            if (a_k && b_k) product_kernel<T, true, true, 128, 128, 2, 2, 4><<<grid, 256, 0, st>>>(a);
+            else if (a_k) product_kernel<T, true, false, 128, 128, 2, 2, 4><<<grid, 256, 0, st>>>(a);
+            else product_kernel<T, false, false, 128, 128, 2, 2, 4><<<grid, 256, 0, st>>>(a);
+            return joined();
+        }
+    if (a_k && b_k) product_kernel<T, true, true, 128, 128, 2, 2, 2><<<grid, 256, 0, st>>>(a);
+    else if (a_k) product_kernel<T, true, false, 128, 128, 2, 2, 2><<<grid, 256, 0, st>>>(a);
+    else product_kernel<T, false, false, 128, 128, 2, 2, 2><<<grid, 256, 0, st>>>(a);
+    joined();
 }
 
 template <typename T>
@@ -77,11 +91,9 @@ extern template void launch_small_back_of<f16>(const SmallBackArgs &, int, int, 
 extern template void launch_product_of<bf16>(const ProductArgs &, const ProductPlan &, bool, bool, hipStream_t);
 extern template void launch_product_of<f16>(const ProductArgs &, const ProductPlan &, bool, bool, hipStream_t);
 
-constexpr int64_t CUS = 256, MOST_SPLITS = 128;
-
 // Microseconds a product takes with tiles of 256 or 128 and its k's split, by the times measured at 16 .. 16384 rows, columns and k's in bf16 and
-// fp32: a tile of 256 has a compute unit to itself, of 128 two share one.  Adding up the splits costs a launch and the sums' way through memory.
-// 4096 x 1664 -> 4096 in bf16: 256 48, 128 54 us; 2048 x 2048 -> 2048: 43 and 27; dw of 16384 x 896 -> 4096: 128 175, split in two 126, 256 split in
+// fp32: a tile of 256 has a compute unit to itself, of 128 two share one if there are so many.  Adding up the splits costs a launch and the sums' way through memory.
+// 4096 x 1664 -> 4096 in bf16: 256 48, 128 54 us; 2048 x 2048 -> 2048: 43 and 20; dw of 16384 x 896 -> 4096: 128 175, split in two 126, 256 split in
 // four 129; dw of 100000 x 64 -> 64: split in 32 34 + 10, in 128 13 + 6.  Tiles of 256 x 128 (two waves' 64 x 64 side by side, one workgroup a compute
 // unit) were slower than one of the two everywhere.
 static double tiles_us(int tile, int64_t tiles, int64_t splits, int64_t steps, int64_t m, int64_t n, bool f32, bool b_k)
@@ -89,7 +101,8 @@ static double tiles_us(int tile, int64_t tiles, int64_t splits, int64_t steps, i
     const double s = (double)((steps + splits - 1) / splits), start = b_k ? 4 : 7;
     const int64_t groups = tiles * splits, turns = (groups + CUS - 1) / CUS;
     double us = 0;
-    if (tile == 256) us = (double)turns * (10 + (f32 ? 7.3 : 1.5) * s);
+    if (tile == 128 && !f32 && groups <= CUS && s >= DEEP_STEPS) us = start + (0.35 + 0.1 * (double)groups / CUS) * s;
+    else if (tile == 256) us = (double)turns * (10 + (f32 ? 7.3 : 1.5) * s);
     else us = (double)(turns / 2) * (start + 2 + (f32 ? 4.1 : 0.8) * s) + (double)(turns % 2) * (start + (f32 ? 2.1 : 0.62) * s);
     return splits > 1 ? us + 3 + (double)splits * (double)m * (double)n * 1.4e-6 : us;
 }

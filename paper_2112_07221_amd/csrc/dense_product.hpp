@@ -285,7 +285,21 @@ __device__ __forceinline__ f32x4 *finish_room(i32x4 *first, i32x4 *second)
 // while a step is multiplied, and nothing passes through registers.  Pieces behind an edge are asked for outside the buffer's range, which
 // reads as zero.  Operands' rows begin at multiples of 16 bytes and are whole pieces wide; others are laid out so first (lay_kernel): pieces taken
 // through registers from rows that begin anywhere cost more (2051 x 3001 -> 2049 in bf16 172 us, laid out 51; in fp32 484 and 275).
-__device__ __forceinline__ void copies_done() { __builtin_amdgcn_s_waitcnt(0x0F70); }        // vmcnt(0) alone
+// The workgroup's barrier between two steps: every wave has its LDS reads in registers (lgkmcnt(0)) and its copies done but for the last N asked
+// for (vmcnt(N)).  __syncthreads() would wait for all copies, those of later steps too; the fences keep the compiler from moving reads or copies
+// across.
+template <int N> __device__ __forceinline__ void step_barrier()
+{
+    static_assert(N < 64, "vmcnt's range");
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_s_waitcnt(0x0070 | (N & 15) | N >> 4 << 14);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_sched_barrier(0);
+}
 
 template <typename T, int R, bool K, bool PERMUTED, int THREADS>
 struct Copy : Tile<T, R, K, PERMUTED> {
@@ -326,14 +340,16 @@ struct Copy : Tile<T, R, K, PERMUTED> {
     }
 };
 
-template <typename T, bool AK, bool BK, int TM, int TN, int WM, int WN>
+template <typename T, bool AK, bool BK, int TM, int TN, int WM, int WN, int STAGES>
 __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
 {
-    constexpr int THREADS = 64 * WM * WN, MI = TM / WM / 32, NI = TN / WN / 32;
+    constexpr int THREADS = 64 * WM * WN, MI = TM / WM / 32, NI = TN / WN / 32, S = STAGES;
+    static_assert(S == 2 || S == 4, "the loop's buffers");
     using CA = Copy<T, TM, AK, false, THREADS>;
     using CB = Copy<T, TN, BK, true, THREADS>;
-    // (arrays of their own, and a loop of two steps: the compiler sees that a step's reads do not wait for the other buffer's copies)
+    // (arrays of their own, and a loop of as many steps: the compiler sees that a step's reads do not wait for the other buffers' copies)
     __shared__ i32x4 a0[CA::PIECES], a1[CA::PIECES], b0[CB::PIECES], b1[CB::PIECES];
+    __shared__ i32x4 a2[S > 2 ? CA::PIECES : 1], a3[S > 2 ? CA::PIECES : 1], b2[S > 2 ? CB::PIECES : 1], b3[S > 2 ? CB::PIECES : 1];
     const int tiles = a.tiles_m * a.tiles_n, split = blockIdx.x / tiles;
     int tm, tn;
     tile_at(tile_of(blockIdx.x % tiles, tiles), a.tiles_m, a.tiles_n, tm, tn);
@@ -362,37 +378,45 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
     // A frag's reads go out before the products of the frag before.  The last frag of a step is in registers before its products start: at that point
     // the buffer is free for the step after the next, and the next step's first frag can be read.  The copies of one operand go out among those
     // last products, the other's among the first ones of the next step: all of them at once held the products up (8192 x 4096 -> 4096 bf16: dw 231 -> 216 us).
-    int left = k_end - k_begin;
-    auto step = [&](i32x4 *la, i32x4 *lb, i32x4 *next_a, i32x4 *next_b) {
+    constexpr int EACH = CA::EACH + CB::EACH, STEP = CA::STEP;
+    int left = k_end - k_begin;                     // from the step's first k on
+    auto step = [&](i32x4 *la, i32x4 *lb, i32x4 *next_a, i32x4 *next_b, i32x4 *before_b) {
         read(la, lb, 1, 1);
-        cb.step(next_b, left);
+        cb.step(before_b, left - (S - 1) * STEP);
         products(0);
         read(la, lb, 2, 0);
         products(1);
         read(la, lb, 3, 1);
         products(0);
-        copies_done();
-        __syncthreads();
-        left -= CA::STEP;
+        step_barrier<(S - 2) * EACH>();
+        left -= STEP;
         read(next_a, next_b, 0, 0);
-        ca.step(la, left);
+        ca.step(la, left - (S - 1) * STEP);
         products(1);
     };
     // Two steps a turn, the last of them perhaps of zeros: with a step of its own behind the loop the compiler keeps the sums twice (and spills).
-    const int steps = (left + CA::STEP - 1) / CA::STEP;
+    const int steps = (left + STEP - 1) / STEP;
     ca.step(a0, left); cb.step(b0, left);
-    copies_done();
-    __syncthreads();
-    left -= CA::STEP;
-    ca.step(a1, left);
+    if constexpr (S > 2) {
+        ca.step(a1, left - STEP); cb.step(b1, left - STEP);
+        ca.step(a2, left - 2 * STEP); cb.step(b2, left - 2 * STEP);
+    }
+    step_barrier<(S - 2) * EACH>();
+    ca.step(S > 2 ? a3 : a1, left - (S - 1) * STEP);
     read(a0, b0, 0, 0);
-    for (int t = 0; t < (steps + 1) / 2; ++t) {
-        step(a0, b0, a1, b1);
-        step(a1, b1, a0, b0);
+    for (int t = 0; t < (steps + S - 1) / S; ++t) {
+        if constexpr (S > 2) {
+            step(a0, b0, a1, b1, b3);
+            step(a1, b1, a2, b2, b0);
+            step(a2, b2, a3, b3, b1);
+            step(a3, b3, a0, b0, b2);
+        } else {
+            step(a0, b0, a1, b1, b1);
+            step(a1, b1, a0, b0, b0);
+        }
     }
     static_assert(NI == 2 && CA::PIECES >= WM * WN / 2 * FINISH_PIECES, "a wave ends 64 columns, in the tiles' LDS");
-    copies_done();                                  // (zeros for a step that does not come)
-    __syncthreads();
+    step_barrier<0>();                              // (zeros for steps that do not come)
     f32x4 *room = finish_room<WM * WN>(a0, a1);
     // (the code once, with the sums moved up: four copies of it are more than the instruction cache holds)
 #pragma unroll 1
