@@ -138,7 +138,8 @@ ForwardPlan forward_plan(const het_linear_t *l)
 {
     ForwardPlan p;
     Room room;
-    p.y = product_plan(l->rows, l->out, l->in, l->type, true, true, product_lies(l->x, l->ldx, l->in, l->type), product_lies(l->w, l->ldw, l->in, l->type));
+    p.y = product_plan(l->rows, l->out, l->in, l->type, true, true, lay_us(product_lies(l->x, l->ldx, l->in, l->type), l->rows, l->in, l->type),
+                       lay_us(product_lies(l->w, l->ldw, l->in, l->type), l->out, l->in, l->type));
     p.partial_at = room.take(p.y.partial_bytes);
     p.x_at = room.take_laid(p.y.lay_a, l->rows, l->in, l->type);
     p.w_at = room.take_laid(p.y.lay_b, l->out, l->in, l->type);
@@ -161,10 +162,11 @@ BackPlan back_plan(const het_linear_t *l)
     const bool dz_lies = product_lies(dz, l->dz ? l->lddz : l->lddy, l->out, l->type);
     p.runs_slope = l->dz || l->dbias;
     p.slope = slope_splits(l->rows, l->out);
-    if (l->dx) p.dx = product_plan(l->rows, l->in, l->out, l->type, true, false, dz_lies, product_lies(l->w, l->ldw, l->in, l->type));
+    const double dz_us = (p.runs_slope ? written_us : lay_us)(dz_lies, l->rows, l->out, l->type);       // (for each product as if it were the only one)
+    if (l->dx) p.dx = product_plan(l->rows, l->in, l->out, l->type, true, false, dz_us, lay_us(product_lies(l->w, l->ldw, l->in, l->type), l->out, l->in, l->type));
     // x in 8 bits is expanded into rows that lie well
     p.ldx = l->xq ? laid_pitch(l->in, l->type) : l->ldx;
-    if (l->dw) p.dw = product_plan(l->out, l->in, l->rows, l->type, false, false, dz_lies, l->xq || product_lies(l->x, l->ldx, l->in, l->type));
+    if (l->dw) p.dw = product_plan(l->out, l->in, l->rows, l->type, false, false, dz_us, lay_us(l->xq || product_lies(l->x, l->ldx, l->in, l->type), l->rows, l->in, l->type));
     p.lay_dz = p.dx.lay_a || p.dw.lay_a;
     p.bias_at = room.take(l->dbias && p.slope > 1 ? (int64_t)p.slope * width_of(l->out) * 4 : 0);
     p.partial_at = room.take(std::max(p.dx.partial_bytes, p.dw.partial_bytes));

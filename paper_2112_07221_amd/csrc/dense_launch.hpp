@@ -30,8 +30,11 @@ struct ProductPlan {
     int64_t partial_bytes;
 };
 
-// D[m][n] over k; `a_k`, `b_k`: the operands are read along k; `lies_a`, `lies_b`: they are as product_lies asks.  type: HET_F32, ...
-ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k, bool lies_a, bool lies_b);
+// D[m][n] over k; `a_k`, `b_k`: the operands are read along k; `lay_a`, `lay_b`: what laying them out takes
+// (us; 0: they are as product_lies asks).  type: HET_F32, ...
+ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k, double lay_a, double lay_b);
+double lay_us(bool lies, int64_t rows, int64_t width, int type);
+double written_us(bool lies, int64_t rows, int64_t width, int type);
 bool product_lies(const void *p, int64_t ld, int64_t width, int type);
 
 // Rows of `width` values as product_kernel takes them: values from a row to the next, and their launch.

@@ -113,19 +113,20 @@ static double tiles_us(int tile, int64_t tiles, int64_t splits, int64_t steps, i
 static double small_us(int64_t steps, int64_t m, int64_t n, int64_t k, bool a_k, bool b_k, bool f32)
 {
     const int64_t high = a_k && b_k && m <= 16 ? 16 : (m + 31) / 32 * 32, wide = (n + 31) / 32 * 32;
-    const double turn = a_k ? 1 : 2, each = f32 ? 28e-9 : a_k && b_k ? 12e-9 : 20e-9;
-    return 1 + turn * (double)((steps + 2 * SMALL_WAVES - 1) / (2 * SMALL_WAVES)) + 4.0 / 1024 * (double)high * (double)wide / 1024 +
+    const double turn = !a_k ? 2.5 : f32 ? 2 : 1.5, each = f32 ? 28e-9 : b_k ? 16e-9 : 20e-9;
+    return 0.5 + turn * (double)((steps + 2 * SMALL_WAVES - 1) / (2 * SMALL_WAVES)) + 4.0 / 1024 * (double)high * (double)wide / 1024 +
            each * (double)high * (double)wide * (double)k;
 }
 
-// ... and laying out an operand: a launch, and its way there and back through memory.
-static double lay_us(int64_t rows, int64_t width, bool f32) { return 3 + (double)rows * (double)width * (f32 ? 8 : 4) / 4e6; }
+// ... and laying out an operand: a launch, and its way there and back through memory; only there if slope_kernel does it.
+double lay_us(bool lies, int64_t rows, int64_t width, int type) { return lies ? 0 : 3 + 2 * written_us(lies, rows, width, type); }
+double written_us(bool lies, int64_t rows, int64_t width, int type) { return lies ? 0 : 0.1 + (double)rows * (double)width * (type == HET_F32 ? 4 : 2) / 4e6; }
 
-ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k, bool lies_a, bool lies_b)
+ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bool b_k, double lay_a, double lay_b)
 {
     const bool f32 = type == HET_F32;
     ProductPlan p{};
-    p.lay_a = !lies_a; p.lay_b = !lies_b;
+    p.lay_a = lay_a > 0; p.lay_b = lay_b > 0;
     p.m = (int)m; p.n = (int)n; p.k = (int)k;
     double best = 1e30;
     const int64_t step = f32 ? 32 : 64, steps = (k + step - 1) / step;
@@ -140,7 +141,7 @@ ProductPlan product_plan(int64_t m, int64_t n, int64_t k, int type, bool a_k, bo
         for (int64_t splits = 1; splits <= most; splits += splits < 8 ? 1 : splits / 4) of(splits);
         for (int64_t turns = 1; turns <= 4 && most > 8; turns *= 2) of(std::max<int64_t>(1, std::min(most, turns * CUS / tiles)));
     }
-    best += (p.lay_a ? lay_us(m, k, f32) : 0) + (p.lay_b ? lay_us(n, k, f32) : 0);
+    best += lay_a + lay_b;
     if (small_us(steps, m, n, k, a_k, b_k, f32) < best) {
         p.small_m = a_k && b_k && m <= 16 ? 1 : 2;
         p.small_n = ((m + 31) / 32) * ((n + 31) / 32) < CUS ? 1 : 2;
@@ -211,7 +212,7 @@ static int64_t small_sizes(ProductArgs &a, const ProductPlan &p)
 bool launch_small_back(ProductArgs dw, const ProductPlan &dw_plan, ProductArgs dx, const ProductPlan &dx_plan, const ColumnSumArgs &bias, int type, hipStream_t st)
 {
     if (dw_plan.small_m != 2 || dx_plan.small_m != 2) return false;
-    SmallBackArgs a{dw, dx, bias, 0, 0};
+    SmallBackArgs a{dw, dx, bias, 0, 0, dx_plan.k > dw_plan.k};
     const int64_t w = small_sizes(a.dw, dw_plan), x = small_sizes(a.dx, dx_plan), b = bias.n ? (bias.sets * bias.width + 15) / 16 : 0;
     if ((w + x + b) * 64 * SMALL_WAVES >= 1ll << 31) return false;
     a.dw_groups = (int)w; a.dx_groups = (int)x;

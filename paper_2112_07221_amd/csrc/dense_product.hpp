@@ -633,17 +633,17 @@ struct SmallBackArgs {
     ProductArgs dw, dx;
     ColumnSumArgs bias;
     int dw_groups, dx_groups;           // workgroups of each; those behind them are the sums'
+    int dx_first;                       // the products' order: the one with the longer sums starts first
 };
 
 template <typename T, int NW, int NX>
 __global__ __launch_bounds__(64 * SMALL_WAVES) void small_back_kernel(SmallBackArgs a)
 {
     __shared__ union { SmallRoom<2, NW> dw; SmallRoom<2, NX> dx; float bias[COLUMN_DEEP][17]; } lds;
-    int block = blockIdx.x;
-    if (block < a.dw_groups) return product_small<T, false, false, 2, NW>(a.dw, block, lds.dw.sums);
-    block -= a.dw_groups;
-    if (block < a.dx_groups) return product_small<T, true, false, 2, NX>(a.dx, block, lds.dx.sums);
-    column_sum<64 * SMALL_WAVES>(a.bias, block - a.dx_groups, lds.bias);
+    const int block = blockIdx.x, dw = block - (a.dx_first ? a.dx_groups : 0), dx = block - (a.dx_first ? 0 : a.dw_groups);
+    if (dw >= 0 && dw < a.dw_groups) product_small<T, false, false, 2, NW>(a.dw, dw, lds.dw.sums);
+    else if (dx >= 0 && dx < a.dx_groups) product_small<T, true, false, 2, NX>(a.dx, dx, lds.dx.sums);
+    else column_sum<64 * SMALL_WAVES>(a.bias, block - a.dw_groups - a.dx_groups, lds.bias);
 }
 
 } // namespace het
