@@ -281,8 +281,8 @@ __device__ __forceinline__ f32x4 *finish_room(i32x4 *first, i32x4 *second)
 }
 
 // ---- aligned operands -------------------------------------------------------------------------------------
-// TM x TN tiles, WM x WN waves.  Memory goes straight to LDS, 16 bytes a lane, one step ahead of the products: the next step's pieces are on their way
-// while a step is multiplied, and nothing passes through registers.  Pieces behind an edge are asked for outside the buffer's range, which
+// TM x TN tiles, WM x WN waves.  Memory goes straight to LDS, 16 bytes a lane, STAGES - 1 steps ahead of the products: the next steps' pieces are on their
+// way while a step is multiplied, and nothing passes through registers.  Pieces behind an edge are asked for outside the buffer's range, which
 // reads as zero.  Operands' rows begin at multiples of 16 bytes and are whole pieces wide; others are laid out so first (lay_kernel): pieces taken
 // through registers from rows that begin anywhere cost more (2051 x 3001 -> 2049 in bf16 172 us, laid out 51; in fp32 484 and 275).
 // The workgroup's barrier between two steps: every wave has its LDS reads in registers (lgkmcnt(0)) and its copies done but for the last N asked
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
         __builtin_amdgcn_sched_barrier(0);
     };
     // A frag's reads go out before the products of the frag before.  The last frag of a step is in registers before its products start: at that point
-    // the buffer is free for the step after the next, and the next step's first frag can be read.  The copies of one operand go out among those
+    // the buffer is free for the step S ahead, and the next step's first frag can be read.  The copies of one operand go out among those
     // last products, the other's among the first ones of the next step: all of them at once held the products up (8192 x 4096 -> 4096 bf16: dw 231 -> 216 us).
     constexpr int EACH = CA::EACH + CB::EACH, STEP = CA::STEP;
     int left = k_end - k_begin;                     // from the step's first k on
@@ -394,7 +394,7 @@ __global__ __launch_bounds__(64 * WM * WN) void product_kernel(ProductArgs a)
         ca.step(la, left - (S - 1) * STEP);
         products(1);
     };
-    // Two steps a turn, the last of them perhaps of zeros: with a step of its own behind the loop the compiler keeps the sums twice (and spills).
+    // S steps a turn, the last of them perhaps of zeros: with a step of its own behind the loop the compiler keeps the sums twice (and spills).
     const int steps = (left + STEP - 1) / STEP;
     ca.step(a0, left); cb.step(b0, left);
     if constexpr (S > 2) {

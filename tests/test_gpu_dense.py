@@ -484,6 +484,62 @@ def test_linear_backward(rows, inp, out, t, ty, kept):
         assert torch.equal(a, b) and torch.equal(same, dy)
 
 
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,inp,out", [(1, 40, 24), (300, 48, 96), (700, 200, 96), (1500, 33, 20)])
+def test_gradients_asked_for_together_or_alone(rows, inp, out, t):
+    """A small layer's gradients come out of one launch; each asked for alone has the same bits.  A captured call repeats them."""
+    g = gen(rows + inp)
+    x, z, dy = rows_in(g, rows, inp, t), rows_in(g, rows, out, t, 2.0), rows_in(g, rows, out, t)
+    w = rows_in(g, out, inp, t, 1 / math.sqrt(inp))
+    dz = torch.empty_like(dy)
+
+    def grads(dx=None, dw=None, db=None):
+        dense.linear_backward(dy, x, w, z, dense.ACT_SILU, dz, dx, dw, db)
+
+    def empty():
+        return torch.empty_like(x), torch.empty_like(w), torch.empty(out, device="cuda")
+
+    (dx, dw, db), (a, b, c) = empty(), empty()
+    grads(dx, dw, db)
+    grads(dx=a)
+    grads(dw=b)
+    grads(db=c)
+    assert torch.equal(dx, a) and torch.equal(dw, b) and torch.equal(db, c)
+    near(db, (D(dy) * slope64("silu", D(z))).sum(0), (D(dy).abs() * act_off(D(z))).sum(0) + (rows + 1) * U * (D(dy) * slope64("silu", D(z))).abs().sum(0), "dbias")
+    for u in (a, b, c):
+        u.fill_(7.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        grads(a, b, c)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        grads(a, b, c)
+    for _ in range(3):
+        for u in (a, b, c):
+            u.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dx, a) and torch.equal(dw, b) and torch.equal(db, c)
+
+
+@pytest.mark.parametrize("t", [BF16, F16, F32])
+@pytest.mark.parametrize("inp", [255, 256, 257, 320, 449, 1000])
+def test_tiles_with_copies_far_ahead(inp, t):
+    """Sums of 4 to 16 steps over few tiles: the copies that are asked for beyond the end read as zero, whatever the step the sum ends in."""
+    g = gen(inp)
+    rows, out = 1100, 700
+    x, w = rows_in(g, rows, inp, t), rows_in(g, out, inp, t, 1 / math.sqrt(inp))
+    x[-1], w[-1] = math.inf, 1.0                                   # (the row behind which the copies go on)
+    y = Guarded(rows, out, t)
+    dense.linear(x, w, None, y.m)
+    a, b = D(x)[:-1], D(w)
+    v, o = a @ b.t(), (2 * inp + 2) * U * (a.abs() @ b.abs().t())
+    near(y.m[:-1], v, o + H(t) * (v.abs() + o) + tiny(t), "y")
+    assert not bool(torch.isfinite(y.m[-1]).any()) and y.untouched()
+
+
 def test_the_shapes_reach_split_sums():
     """(300, 8200, 200) is added up from splits (bias, residual, kept z and activation come behind them), forward and in dw's long sum over rows."""
     assert dense.linear_workspace(300, 8200, 200, BF16) > 0
