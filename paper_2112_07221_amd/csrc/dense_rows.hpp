@@ -120,7 +120,7 @@ __global__ __launch_bounds__(MOST) void norm_kernel(NormArgs a)
         f32x8 h;
 #pragma unroll
         for (int j = 0; j < 8; ++j) h[j] = v[i][j] * rstd;
-        if (a.q && c * CHUNK < a.s.pitch) pack_chunk(a.q + row * a.s.pitch, a.e + row * (a.s.pitch / PACK_BLOCK), c, chunk_own<WHOLE>(h, c, dim));
+        if (a.q && c * CHUNK < a.s.pitch) pack_chunk(a.q + row * a.s.pitch, a.e + row * (a.s.pitch / PACK_BLOCK), c, h, WHOLE ? 0 : chunk_skip(c, dim));
         if (n <= 0) continue;
         const f32x8 g = a.gamma ? load_row<WHOLE>(a.gamma, c, dim) : f32x8{1, 1, 1, 1, 1, 1, 1, 1};
         const f32x8 b = a.beta ? load_row<WHOLE>(a.beta, c, dim) : f32x8{};
@@ -257,11 +257,13 @@ __global__ __launch_bounds__(MOST) void norm_back_kernel(NormBackArgs a)
         for (int j = 0; j < 8; ++j) { dg[0][j] += __shfl_xor(dg[0][j], o); db[0][j] += __shfl_xor(db[0][j], o); }
     const bool mine = (int)threadIdx.x % 64 < lanes && gl * CHUNK < width;
     f32x4 *at = reinterpret_cast<f32x4 *>(cols) + 4 * gl;
+    // (before the waves take turns: 333 x 260 7.6 -> 5.7 us)
+    const f32x8 own[2] = {chunk_own<WHOLE>(dg[0], gl, dim), chunk_own<WHOLE>(db[0], gl, dim)};
     for (int w = 0; w < ROW_WAVES; ++w) {
         if ((int)threadIdx.x / 64 == w && mine) {
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const f32x8 s = chunk_own<WHOLE>(u < 2 ? dg[0] : db[0], gl, dim);
+                const f32x8 s = own[u / 2];
                 f32x4 v = {s[4 * (u % 2)], s[4 * (u % 2) + 1], s[4 * (u % 2) + 2], s[4 * (u % 2) + 3]};
                 if (w) for (int j = 0; j < 4; ++j) v[j] += at[u][j];
                 at[u] = v;

@@ -289,12 +289,13 @@ __device__ __forceinline__ uint32_t chunk_magnitude(f32x8 f)
 }
 
 // Writes this lane's chunk of a row's 8-bit form and, by the first of a block's four lanes, the block's step.  All four lanes are active; values
-// behind the row's end come as zero.
-__device__ __forceinline__ void pack_chunk(int8_t *q, uint8_t *e, int c, f32x8 f)
+// behind the row's end come as zero.  `skip`: chunk_skip's, the first values that are not the chunk's own and come as zero (moving bytes costs an eighth
+// of moving values: 30000 x 300 kept 22.3 -> 19.1 us).
+__device__ __forceinline__ void pack_chunk(int8_t *q, uint8_t *e, int c, f32x8 f, int skip = 0)
 {
     const PackStep s = pack_step(quad_max(chunk_magnitude(f)));
-    const uint2 w = {pack_four(f[0], f[1], f[2], f[3], s), pack_four(f[4], f[5], f[6], f[7], s)};
-    *reinterpret_cast<uint2 *>(q + (size_t)c * CHUNK) = w;
+    const uint64_t w = (uint64_t)pack_four(f[4], f[5], f[6], f[7], s) << 32 | pack_four(f[0], f[1], f[2], f[3], s);
+    *reinterpret_cast<uint64_t *>(q + (size_t)c * CHUNK) = skip < CHUNK ? w >> (8 * skip) : 0;
     if ((c & 3) == 0) e[c >> 2] = (uint8_t)s.byte;
 }
 
