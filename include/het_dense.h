@@ -127,7 +127,8 @@ int het_linear(const het_linear_t *l, void *hip_stream);
 /*
  * dz = dy act'(z), rounded to `type`; dbias = column sums of dz before that rounding; dx = dz w; dw = dz^T x.
  * z or zq/ze as het_linear kept it (act == HET_ACT_NONE reads neither).  The input is x, or xq/xe: then it is expanded into the
- * workspace as het_expand does.  relu's slope at 0 is 0.  dz may be NULL if it would be dy itself (no activation, y_type == type), and
+ * workspace as het_expand does.  relu's slope at 0 is 0; an infinite z (a sum
+ * beyond fp16's range kept in fp16) has its slope's limit, 1 or 0.  dz may be NULL if it would be dy itself (no activation, y_type == type), and
  * may be dy itself if the types are the same.  With rows == 0, dw and dbias are zero.
  * workspace: het_linear_workspace(l, 1) bytes, aligned to 16.  HET_EINVAL as above.
  */

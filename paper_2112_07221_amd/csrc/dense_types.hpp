@@ -188,15 +188,17 @@ __device__ __forceinline__ float act_value(int act, float v)
     }
 }
 
+// A sum beyond a 16-bit type's range is kept as an infinity: its slope is the limit, 0 or 1.  So the factor of what vanishes there is held within a range beyond
+// which it has vanished in fp32 (infinity times 0 is a NaN); a NaN stays one by the other factors.
 __device__ __forceinline__ float act_slope(int act, float v)
 {
     switch (act) {
     case DENSE_ACT_RELU: return v > 0.f ? 1.f : v == v ? 0.f : v;
     case DENSE_ACT_GELU: {
         const float tail = normal_tail(v, within_seven(v)), bell = __builtin_amdgcn_exp2f(v * -0.72134752044448170f * v);
-        return fmaf(v * 0.39894228040143268f, bell, v < 0.f ? tail : 1.f - tail);
+        return fmaf(__builtin_amdgcn_fmed3f(v, -16.f, 16.f) * 0.39894228040143268f, bell, v < 0.f ? tail : 1.f - tail);
     }
-    case DENSE_ACT_SILU: { const float p = __builtin_amdgcn_rcpf(1.f + exp_of(-v)); return p * (1.f + v * (1.f - p)); }
+    case DENSE_ACT_SILU: { const float p = __builtin_amdgcn_rcpf(1.f + exp_of(-v)); return p * (1.f + __builtin_amdgcn_fmed3f(v, -128.f, 128.f) * (1.f - p)); }
     default: return 1.f;
     }
 }

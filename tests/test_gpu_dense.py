@@ -847,3 +847,50 @@ def test_two_streams_at_once():
     dense.linear(a, w, None, y, stream=s)
     s.synchronize()
     assert bool((y == 4000).all())
+
+
+# ---- sums beyond the type's range --------------------------------------------------------------------------
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+def test_slopes_at_infinity(t, act):
+    """A kept z that is infinite has the slope's limit, 1 or 0: not the NaN of infinity times nothing.  A NaN stays one.  (rows of whole chunks and odd ones)"""
+    for out in (24, 13):
+        g = gen(out)
+        z, dy = rows_in(g, 9, out, t, 2.0), rows_in(g, 9, out, t)
+        z[:, 0], z[:, 5], z[4, 9] = math.inf, -math.inf, math.nan
+        x, w = rows_in(g, 9, 10, t), rows_in(g, out, 10, t)
+        dz, dx, dw, db = torch.empty_like(dy), torch.empty_like(x), torch.empty_like(w), torch.empty(out, device="cuda")
+        dense.linear_backward(dy, x, w, z, ACTS[act], dz, dx, dw, db)
+        assert torch.equal(dz[:, 0], dy[:, 0]) and bool((dz[:, 5] == 0).all())
+        assert bool(torch.isnan(dz[4, 9]))
+        nan = torch.zeros_like(dz, dtype=torch.bool)
+        nan[4, 9] = True
+        assert bool(torch.isfinite(dz[~nan]).all())
+        assert bool(torch.isnan(dx[4]).all()) and bool(torch.isfinite(torch.cat((dx[:4], dx[5:]))).all())
+        assert bool(torch.isnan(dw[9]).all()) and bool(torch.isfinite(torch.cat((dw[:9], dw[10:]))).all())
+        assert bool(torch.isnan(db[9])) and bool(torch.isfinite(torch.cat((db[:9], db[10:]))).all())
+
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+@pytest.mark.parametrize("ty", [F16, F32])
+@pytest.mark.parametrize("rows", [40, 300])
+def test_sums_beyond_fp16_kept_in_fp16(rows, ty, act):
+    """Two units whose sums are +-72000: kept as infinities, their outputs (0, and 72000 in fp32) and every gradient are what they would be."""
+    g = gen(rows)
+    x, w = torch.ones(rows, 8), torch.randn(20, 8, generator=g)
+    w[3], w[4] = 9000.0, -9000.0
+    x, w, dy = x.to(F16).cuda(), w.to(F16).cuda(), rows_in(g, rows, 20, ty, 0.01)
+    y, z = torch.empty(rows, 20, dtype=ty, device="cuda"), torch.empty(rows, 20, dtype=F16, device="cuda")
+    dense.linear(x, w, None, y, ACTS[act], z=z)
+    assert bool((z[:, 3] == math.inf).all()) and bool((z[:, 4] == -math.inf).all())
+    assert bool((y[:, 3] == (math.inf if ty is F16 else 72000.0)).all()) and bool((y[:, 4] == 0).all())
+    dz, dx, dw, db = torch.empty_like(z), torch.empty_like(x), torch.empty_like(w), torch.empty(20, device="cuda")
+    dense.linear_backward(dy, x, w, z, ACTS[act], dz, dx, dw, db)
+    want = D(dy) * slope64(act, D(z).clamp(-1e3, 1e3))
+    off = D(dy).abs() * act_off(D(z).clamp(-20, 20)) + U * want.abs()
+    near(dz, want, off + H(F16) * (want.abs() + off) + tiny(F16), "dz")
+    near(db, want.sum(0), rows * U * want.abs().sum(0) + off.sum(0), "dbias")
+    h = D(dz)
+    for got, a, b, what in ((dx, h, D(w), "dx"), (dw, h.t(), D(x), "dw")):
+        v, o = a @ b, (2 * a.shape[1] + 2) * U * (a.abs() @ b.abs())
+        near(got, v, o + H(F16) * (v.abs() + o) + tiny(F16), what)
