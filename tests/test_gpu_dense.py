@@ -894,3 +894,56 @@ def test_sums_beyond_fp16_kept_in_fp16(rows, ty, act):
     for got, a, b, what in ((dx, h, D(w), "dx"), (dw, h.t(), D(x), "dw")):
         v, o = a @ b, (2 * a.shape[1] + 2) * U * (a.abs() @ b.abs())
         near(got, v, o + H(F16) * (v.abs() + o) + tiny(F16), what)
+
+
+# ---- the functions themselves ------------------------------------------------------------------------------
+# gelu's negative part is |v| Phi(-|v|), with Phi(-x) = exp2(E), E = -x^2 / 2 log2(e) + q(x) and q a polynomial in x up to 8.  Relative to it: the fit is off by at most 6.1e-7.
+# E: two roundings and the constant's of 0.72 x^2, E's own (E < 0.73 x^2 + 6); Horner's rule for q, by the running bound (the sum of every step's result times the power it
+# is still multiplied by), 1, 3.1, 5.3, 8.3, 14.3, 30.1, 76.6, 210, 567 U at x = 0 .. 8; all of that times ln 2; exp2 1 ulp and the products: below U (10 + 3 x^2 + 1.5 2^x).
+# Beyond 8, 8 Phi'(v) stands for |v| Phi(v), where Phi' goes on with q(8): x R(x), R(x) = Phi(-x) exp(x^2 / 2), grows by less than 1 / 64 from there on.
+def gelu_tail_off(v):
+    x = v.abs()
+    near8 = x.clamp(max=8.0)
+    return U * (10 + 3 * x * x + 1.5 * torch.exp2(near8)) + 6.1e-7 + torch.where(x > 8, 1 / 64, 0.0)
+
+
+def lower_tail(v):
+    """Phi(v) in 64 bits for negative v too (torch.special.ndtr is (1 + erf) / 2, which has lost half of its digits at -6 and all at -8.5)."""
+    return torch.special.erfc(-v * 0.5 ** 0.5) / 2
+
+
+# silu: exp's argument is off by 2 ulp of it, the exponential, the sum, the reciprocal and the product by 1 each: the sigmoid p is off by U (8 + 2.1 |v|) of it where v is
+# negative, by 5 U otherwise.  Its slope p (1 + v (1 - p)): that times 1 + |v|, and the roundings of 1 - p and the products.
+def sigmoid_off(v):
+    return torch.where(v < 0, U * (8 + 2.1 * v.abs()), 5 * U)
+
+
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_activations_over_their_range(act, t):
+    """Values and slopes on a grid, against 64 bits: down the negative tail to where the type ends, and small arguments."""
+    v = torch.cat((torch.linspace(-14, 14, 28 * 2048 + 1), -torch.logspace(-20, 0, 500), torch.logspace(-20, 0, 500), torch.tensor([0.0, 8.0, -8.0, 30.0, -30.0])))
+    least = 2.0 ** -126                     # an exponential below it may be zero; gelu's are multiplied by at most 8
+    # values: of zero steps plus a weight, which is exactly the argument
+    y = torch.empty(1, v.numel(), dtype=t, device="cuda")
+    p = dense.Packed(torch.zeros(1, pitch(v.numel()), dtype=torch.int8, device="cuda"), torch.full((1, pitch(v.numel()) // 32), 127, dtype=torch.uint8, device="cuda"), v.numel())
+    dense.expand(p, y, ACTS[act], None, v.cuda())
+    v64 = D(v)
+    want = (v64 * lower_tail(v64) if act == "gelu" else act64(act, v64))[None]
+    off = (v64.abs() * lower_tail(-v64.abs()) * gelu_tail_off(v64) if act == "gelu" else want.abs() * sigmoid_off(v64)) + U * want.abs() + 8 * least
+    near(y, want, off + H(t) * (want.abs() + off) + tiny(t), "values")
+    # slopes: of arguments in the layer's type, with a gradient of ones
+    z = v.to(t).cuda().view(1, -1)
+    dz = torch.empty_like(z)
+    dense.linear_backward(torch.ones_like(z), None, torch.zeros(z.shape[1], 1, dtype=t, device="cuda"), z, ACTS[act], dz, None, None)
+    z64 = D(z)
+    want, x = slope64(act, z64), z64.abs()
+    if act == "gelu":
+        bell = x * torch.exp(-x * x / 2) / math.sqrt(2 * math.pi)
+        tail = lower_tail(-x)
+        want = lower_tail(z64) + torch.sign(z64) * bell
+        off = tail * (gelu_tail_off(z64) + torch.where(x > 8, 1.0, 0.0)) + bell * U * (8 + 2.2 * x * x) + 2 * U * (want.abs() + torch.where(z64 < 0, 0.0, 1.0)) + 8 * least
+    else:
+        s = torch.sigmoid(z64)
+        off = s * (sigmoid_off(z64) + 4 * U) * (1 + x) + U * want.abs() + 100 * least          # (p below it, times 1 + |v|)
+    near(dz, want, off + H(t) * (want.abs() + off) + tiny(t), "slopes")
