@@ -947,3 +947,27 @@ def test_activations_over_their_range(act, t):
         s = torch.sigmoid(z64)
         off = s * (sigmoid_off(z64) + 4 * U) * (1 + x) + U * want.abs() + 100 * least          # (p below it, times 1 + |v|)
     near(dz, want, off + H(t) * (want.abs() + off) + tiny(t), "slopes")
+
+
+
+# ---- z kept in both forms ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("t", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,inp,out", [(9, 200, 65), (33, 200, 65), (2048, 512, 1000), (2048, 512, 1024), (300, 8200, 200)])
+def test_z_kept_whole_and_in_8_bits_at_once(rows, inp, out, t):
+    """One call of the C entry may write both; the same bits as two calls.  Few rows, a small product, tiles with edges and without, split sums."""
+    g = gen(rows + out)
+    x, w = rows_in(g, rows, inp, t), rows_in(g, out, inp, t, 1 / math.sqrt(inp))
+    bias, r = torch.randn(out, generator=g).cuda(), rows_in(g, rows, out, F32)
+    want, want_z, want_p = torch.empty(rows, out, device="cuda"), torch.empty(rows, out, dtype=t, device="cuda"), dense.Packed.empty(rows, out)
+    dense.linear(x, w, bias, want, dense.ACT_GELU, r, z=want_z)
+    dense.linear(x, w, bias, want, dense.ACT_GELU, r, z=want_p)
+    y, z, p = Guarded(rows, out, F32), Guarded(rows, out, t), dense.Packed.empty(rows, out)
+    need = dense.linear_workspace(rows, inp, out, t)
+    ws = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    kind = {F32: dense.F32, BF16: dense.BF16, F16: dense.F16}[t]
+    l = dense.linear_struct(rows=rows, inp=inp, out=out, type=kind, y_type=dense.F32, act=dense.ACT_GELU, x=x.data_ptr(), ldx=inp, w=w.data_ptr(), ldw=inp, bias=bias.data_ptr(),
+                            residual=r.data_ptr(), ld_residual=out, y=y.m.data_ptr(), ldy=y.m.stride(0), z=z.m.data_ptr(), ldz=z.m.stride(0), zq=p.q.data_ptr(), ze=p.e.data_ptr(),
+                            workspace=ws.data_ptr(), workspace_bytes=need)
+    assert dense.load().het_linear(l, torch.cuda.current_stream().cuda_stream) == 0
+    assert torch.equal(y.m, want) and torch.equal(z.m, want_z) and torch.equal(p.q, want_p.q) and torch.equal(p.e, want_p.e)
+    assert y.untouched() and z.untouched()
