@@ -31,18 +31,23 @@ HBM_PEAK_GBPS = 8000.0       # MI355X published HBM3E bandwidth
 TRAFFIC_FILE = os.path.join(ROOT, "profiles", "hbm_traffic.json")
 
 
-def measured_traffic(kernel, config, build_id):
+def measured_traffic(kernel, config):
     """HBM bytes per launch (fetch + write) of `kernel` on workload `config`, from the rocprofv3
     FETCH_SIZE / WRITE_SIZE counter runs recorded in profiles/hbm_traffic.json (scaled there by a
-    256 MiB device copy of the same run).  The record names the build it was measured on; for any
-    other build of the library, or a workload that was not measured, the answer is None."""
+    256 MiB device copy of the same run).  The record names the cache's sources it was measured on
+    (build.cache_id()); for other ones, a library that was not built from this tree, or a workload
+    that was not measured, the answer is None."""
+    from paper_2112_07221_amd import build
+    from paper_2112_07221_amd import hetcache as hc
+    if hc.build_id() != build.source_id():
+        return None
     try:
         with open(TRAFFIC_FILE) as fh:
             rec = json.load(fh)
     except (OSError, ValueError):
         return None
     entry = rec.get(f"config{config}", {})
-    if entry.get("build_id") != build_id:
+    if entry.get("cache_id") != build.cache_id():
         return None
     return entry.get("bytes_per_launch", {}).get(kernel)
 
@@ -497,7 +502,7 @@ def main():
         achieved = dom_bytes / (kern[dominant]["avg_us"] * 1e-6) / 1e9
         roofline = {"bound": "hbm", "kernel": dominant, "achieved": achieved, "peak": HBM_PEAK_GBPS,
                     "unit": "GB/s", "frac": achieved / HBM_PEAK_GBPS,
-                    "traffic": measured_traffic(dominant, w.index, hc.build_id()),
+                    "traffic": measured_traffic(dominant, w.index),
                     "bytes_per_launch": dom_bytes, "avg_us": kern[dominant]["avg_us"]}
     step_bytes, least_bytes = algorithmic_bytes(w, per_step), algorithmic_bytes(w, per_step, separate=False)
 

@@ -22,16 +22,24 @@ FLAGS = [
 ]
 
 
-def source_id() -> str:
-    """Short hash of the sources the library is built from (the headers and everything in csrc/):
-    what `het_build_id()` returns, so that a measurement can name the build it was taken on."""
+def _hash(headers, sources) -> str:
     h = hashlib.sha256()
-    files = [os.path.join(HERE, "..", "include", h) for h in ("het_cache.h", "het_dense.h")]
-    files += sorted(os.path.join(HERE, "csrc", f) for f in os.listdir(os.path.join(HERE, "csrc")))
-    for f in files:
+    for f in [os.path.join(HERE, "..", "include", n) for n in headers] + [os.path.join(CSRC, n) for n in sources]:
         with open(f, "rb") as fh:
             h.update(fh.read())
     return h.hexdigest()[:12]
+
+
+def source_id() -> str:
+    """Short hash of the sources the library is built from (the headers and everything in csrc/):
+    what `het_build_id()` returns, so that a measurement can name the build it was taken on."""
+    return _hash(("het_cache.h", "het_dense.h"), sorted(os.listdir(CSRC)))
+
+
+def cache_id() -> str:
+    """The same of the cache's sources alone (without csrc/dense*, which none of them includes): a measurement of the
+    cache's kernels holds for every build that has them."""
+    return _hash(("het_cache.h",), sorted(n for n in os.listdir(CSRC) if not n.startswith("dense")))
 
 
 def build(verbose: bool = False, flags=()) -> str:
