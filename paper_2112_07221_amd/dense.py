@@ -369,6 +369,7 @@ class ResidualBlock:
 
     def forward(self, x, y):
         """y of x, both float32 [rows, dim]; x has to stay until backward if activations are kept whole."""
+        self._ready = False                                # (a call that is refused half way leaves nothing for backward)
         layer_norm(x, self.gamma, self.beta, self._h, self._mean, self._rstd, packed=self._n8, eps=self.eps)
         linear(self._h, self.w1, self.b1, self._u, self.act, z=self._z, workspace=self._workspace)
         linear(self._u, self.w2, self.b2, y, residual=x, workspace=self._workspace)

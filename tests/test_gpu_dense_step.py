@@ -136,3 +136,20 @@ def test_the_gradient_may_take_the_place_of_the_outputs():
     assert torch.equal(dx, dy)
     with pytest.raises(RuntimeError):                     # once for a forward pass
         b.backward(dy, dx)
+
+
+@pytest.mark.parametrize("keep8", [False, True])
+def test_a_refused_forward_pass_leaves_nothing_for_backward(keep8):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(4)
+    b = dense.ResidualBlock(20, 40, 64, torch.bfloat16, keep8=keep8, generator=g)
+    x, y, dy, dx = [torch.randn(20, 40, generator=g, device="cuda") for _ in range(4)]
+    b.forward(x, y)
+    with pytest.raises(TypeError):
+        b.forward(x, y.double())                          # refused by the last layer: what was kept is of the new x already
+    with pytest.raises(RuntimeError):
+        b.backward(dy, dx)
+    b.forward(x, y)
+    b.backward(dy, dx)
+    with pytest.raises(RuntimeError):
+        b.backward(dy, dx)
