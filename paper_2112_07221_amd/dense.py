@@ -328,15 +328,34 @@ def linear_backward(dy, x, w, z, act, dz, dx, dw, dbias=None, x_act=ACT_NONE, x_
                                 _stream(stream, dev)), "het_linear_backward")
 
 
+class BlockScratch:
+    """What a ResidualBlock needs only while one of its passes runs: the layers' inputs and their gradients (rows x (dim + hidden) values) and the calls' workspace.
+    Blocks of these sizes that run one after the other on one stream may share one; a captured pass writes to it at every replay.
+
+    keep8: for blocks that keep their activations in 8 bits too (the workspace has room for a layer's input made from them)."""
+
+    def __init__(self, rows, dim, hidden, dtype=None, keep8=True, device="cuda"):
+        load()
+        import torch
+        self.rows, self.dim, self.hidden, self.keep8 = rows, dim, hidden, keep8
+        dtype = self.dtype = dtype or torch.bfloat16
+        self.h, self.u = torch.empty(rows, dim, dtype=dtype, device=device), torch.empty(rows, hidden, dtype=dtype, device=device)
+        need = max([linear_workspace(rows, dim, hidden, dtype), linear_workspace(rows, hidden, dim, dtype), layer_norm_workspace(rows, dim), 16] +
+                   [linear_workspace(rows, i, o, dtype, True, packed) for i, o in ((dim, hidden), (hidden, dim)) for packed in ((False, True) if keep8 else (False,))])
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
+
+
 class ResidualBlock:
     """y = x + w2 act(w1 norm(x) + b1) + b2 over rows of `dim` values with `hidden` values inside, in a float32 residual stream: what
     stands between the rows a lookup hands out (x) and the gradient an update takes (dx).  Weights and what is multiplied are of `dtype`.
 
-    keep8: between the passes the normalised rows and the pre-activations are kept in 8 bits (8.25 bits a value; the layers' inputs are made
-    from them again), else x, mean, rstd, the normalised rows with their weights, z and act(z) are kept whole.  Buffers and the workspace are the
-    block's own and are taken at construction: calls allocate nothing, and a block is used on one stream at a time."""
+    keep8: between the passes the normalised rows and the pre-activations are kept in 8 bits (8.25 bits a value, and rstd; the layers' inputs are made
+    from them again), else mean, rstd, the normalised rows with their weights, z and act(z) are kept whole, and x by the caller.  At 4096 rows of 1664
+    values, 4096 inside, in bf16: 24 MB, or 81 and x's 27.  What is needed within a pass alone, 47 MB and a workspace of 35 (7 for blocks that keep
+    whole), is in `scratch`: one BlockScratch for any number of blocks that run one after the other, or the block's own (None).  All is taken at construction: calls allocate nothing, and a
+    block is used on one stream at a time."""
 
-    def __init__(self, rows, dim, hidden, dtype=None, act=ACT_GELU, eps=1e-5, keep8=True, generator=None, device="cuda"):
+    def __init__(self, rows, dim, hidden, dtype=None, act=ACT_GELU, eps=1e-5, keep8=True, generator=None, device="cuda", scratch=None):
         load()
         import torch
         self.rows, self.dim, self.hidden, self.act, self.eps, self.keep8 = rows, dim, hidden, act, eps, keep8
@@ -352,16 +371,17 @@ class ResidualBlock:
         self.dgamma, self.dbeta, self.dw1, self.dw2 = new(dim), new(dim), new(hidden, dim, dtype=dtype), new(dim, hidden, dtype=dtype)
         self.db1, self.db2 = new(hidden), new(dim)
         # between the passes
-        self._h, self._u = new(rows, dim, dtype=dtype), new(rows, hidden, dtype=dtype)
-        self._mean, self._rstd, self._x, self._ready = new(rows), new(rows), None, False
+        self._rstd, self._x, self._ready = new(rows), None, False
+        self._mean = None if keep8 else new(rows)
         self._n8 = Packed.empty(rows, dim, device) if keep8 else None
         self._z = Packed.empty(rows, hidden, device) if keep8 else new(rows, hidden, dtype=dtype)
-        # backward (the forward pass' h and u are free by then if they were kept in 8 bits)
-        self._dz2 = new(rows, dim, dtype=dtype)
-        self._du, self._dh = (self._u, self._h) if keep8 else (new(rows, hidden, dtype=dtype), new(rows, dim, dtype=dtype))
-        need = max(linear_workspace(rows, dim, hidden, dtype), linear_workspace(rows, hidden, dim, dtype), layer_norm_workspace(rows, dim), 16,
-                   linear_workspace(rows, dim, hidden, dtype, True, keep8), linear_workspace(rows, hidden, dim, dtype, True, keep8))
-        self._workspace = new(need, dtype=torch.uint8)
+        # within one
+        scratch = scratch or BlockScratch(rows, dim, hidden, dtype, keep8, device)
+        if (scratch.rows, scratch.dim, scratch.hidden, scratch.dtype) != (rows, dim, hidden, dtype) or scratch.keep8 < keep8:
+            raise ValueError("the scratch is for blocks of other sizes or another type, or for ones that keep their activations whole")
+        self._dh, self._du, self._workspace = scratch.h, scratch.u, scratch.workspace
+        # (the forward pass' h and u are free when it ends if they are kept in 8 bits)
+        self._h, self._u = (scratch.h, scratch.u) if keep8 else (new(rows, dim, dtype=dtype), new(rows, hidden, dtype=dtype))
 
     def parameters(self):
         """[(parameter, gradient)]; the gradients are written by backward."""
@@ -381,7 +401,8 @@ class ResidualBlock:
         if not self._ready:
             raise RuntimeError("backward follows a forward pass")
         self._ready = False
-        linear_backward(dy, self._z if keep8 else self._u, self.w2, None, ACT_NONE, self._dz2, self._du, self.dw2, self.db2,
+        # dz2 lies where dh will
+        linear_backward(dy, self._z if keep8 else self._u, self.w2, None, ACT_NONE, self._dh, self._du, self.dw2, self.db2,
                         x_act=self.act if keep8 else ACT_NONE, workspace=self._workspace)
         # dz1 takes du's place: slope and product follow each other
         linear_backward(self._du, self._n8 if keep8 else self._h, self.w1, self._z, self.act, self._du, self._dh, self.dw1, self.db1,

@@ -153,3 +153,45 @@ def test_a_refused_forward_pass_leaves_nothing_for_backward(keep8):
     b.backward(dy, dx)
     with pytest.raises(RuntimeError):
         b.backward(dy, dx)
+
+
+@pytest.mark.parametrize("keep8", [False, True])
+def test_stacked_blocks_share_what_a_pass_alone_needs(keep8):
+    """Three blocks one after the other with one scratch: the bits of blocks with scratch of their own; each keeps what it says and no more."""
+    rows, dim, hidden, t = 300, 96, 416, torch.bfloat16
+    dev = torch.device("cuda:0")
+
+    def stack(scratch):
+        g = torch.Generator(device=dev)
+        g.manual_seed(6)
+        return [dense.ResidualBlock(rows, dim, hidden, t, keep8=keep8, generator=g, scratch=scratch) for _ in range(3)]
+
+    def run(blocks):
+        g = torch.Generator(device=dev)
+        g.manual_seed(7)
+        x, grad = [torch.randn(rows, dim, generator=g, device=dev) for _ in range(2)]
+        xs = [x]
+        for b in blocks:
+            xs.append(torch.empty_like(x))
+            b.forward(xs[-2], xs[-1])
+        for b in blocks[::-1]:
+            b.backward(grad, grad)
+        return xs + [grad] + [d.clone() for b in blocks for _, d in b.parameters()]
+
+    want = run(stack(None))
+    scratch = dense.BlockScratch(rows, dim, hidden, t, keep8)
+    before = torch.cuda.memory_allocated()
+    blocks = stack(scratch)
+    parts = sum(v.numel() * v.element_size() for b in blocks for pair in b.parameters() for v in pair)
+    kept = rows * ((dim + hidden) * 33 // 32 + 4 if keep8 else (dim + 2 * hidden) * 2 + 8)
+    assert torch.cuda.memory_allocated() - before <= parts + 3 * (kept + 20 * 512)          # (torch rounds each of a block's tensors up to 512 bytes)
+    for got, w in zip(run(blocks), want):
+        assert torch.equal(got, w)
+    for bad in (dict(rows=rows + 1), dict(dim=dim + 8), dict(hidden=hidden - 8), dict(dtype=torch.float16)):
+        a = {**dict(rows=rows, dim=dim, hidden=hidden, dtype=t), **bad}
+        with pytest.raises(ValueError):
+            dense.ResidualBlock(**a, keep8=keep8, scratch=scratch)
+    if not keep8:
+        with pytest.raises(ValueError):
+            dense.ResidualBlock(rows, dim, hidden, t, keep8=True, scratch=scratch)
+        dense.ResidualBlock(rows, dim, hidden, t, keep8=False, scratch=dense.BlockScratch(rows, dim, hidden, t))
