@@ -209,7 +209,7 @@ int het_layer_norm_backward(const void *dy, int32_t y_type, int64_t lddy, const 
                             int64_t rows, int32_t dim, void *workspace, int64_t workspace_bytes, void *hip_stream)
 {
     if (!norm_sizes(rows, dim) || !known_pair(x_type, y_type) || lddy < dim || lddx < dim || !q != !e) return HET_EINVAL;
-    if ((!q && ldx < dim) || (residual && ld_residual < dim)) return HET_EINVAL;
+    if ((rows > 0 && !q && ldx < dim) || (residual && ld_residual < dim)) return HET_EINVAL;
     const hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (rows > 0 && (!dy || !dx || !rstd || (!q && (!x || !mean)) || !aligned16(q))) return HET_EINVAL;
     if (!workspace_ok(workspace, workspace_bytes, het_layer_norm_workspace(rows, dim))) return HET_EINVAL;

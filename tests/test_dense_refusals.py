@@ -128,3 +128,10 @@ def test_the_binding_refuses_what_is_not_on_the_gpu():
                  lambda: dense.linear(x, x, None, x), lambda: dense.linear_backward(x, x, x, None, 0, None, x, x), lambda: dense.pack(None, p), lambda: dense.pack(v, p)):
         with pytest.raises(TypeError):
             call()
+
+
+def test_layer_norm_backward_of_no_rows_kept_in_8_bits():
+    """What is kept of no rows has no address, and x is not given."""
+    lib = dense.load()
+    assert back(lib, rows=0, dy=None, x=None, ldx=0, dx=None, mean=None, rstd=None, dgamma=None, dbeta=None) == HET_OK
+    assert back(lib, rows=1, ldx=0) == HET_EINVAL

@@ -971,3 +971,9 @@ def test_z_kept_whole_and_in_8_bits_at_once(rows, inp, out, t):
     assert dense.load().het_linear(l, torch.cuda.current_stream().cuda_stream) == 0
     assert torch.equal(y.m, want) and torch.equal(z.m, want_z) and torch.equal(p.q, want_p.q) and torch.equal(p.e, want_p.e)
     assert y.untouched() and z.untouched()
+
+
+def test_norm_gradients_without_rows_kept_in_8_bits_are_zero():
+    e, dg, db = torch.empty(0, 40, device="cuda"), torch.full((40,), 5.0, device="cuda"), torch.full((40,), 5.0, device="cuda")
+    dense.layer_norm_backward(e, dense.Packed.empty(0, 40), None, None, torch.empty(0, device="cuda"), e, dg, db)
+    assert bool((dg == 0).all()) and bool((db == 0).all())
