@@ -352,8 +352,9 @@ class ResidualBlock:
     keep8: between the passes the normalised rows and the pre-activations are kept in 8 bits (8.25 bits a value, and rstd; the layers' inputs are made
     from them again), else mean, rstd, the normalised rows with their weights, z and act(z) are kept whole, and x by the caller.  At 4096 rows of 1664
     values, 4096 inside, in bf16: 24 MB, or 81 and x's 27.  What is needed within a pass alone, 47 MB and a workspace of 35 (7 for blocks that keep
-    whole), is in `scratch`: one BlockScratch for any number of blocks that run one after the other, or the block's own (None).  All is taken at construction: calls allocate nothing, and a
-    block is used on one stream at a time."""
+    whole), is in `scratch`: one BlockScratch for any number of blocks that run one after the other, or the block's own (None).  All is taken at construction, for
+    `rows` rows: passes of so many allocate nothing, ones of fewer rows (the last batch of an epoch) take their workspace from torch's allocator.  A block is used
+    on one stream at a time."""
 
     def __init__(self, rows, dim, hidden, dtype=None, act=ACT_GELU, eps=1e-5, keep8=True, generator=None, device="cuda", scratch=None):
         load()
@@ -371,42 +372,50 @@ class ResidualBlock:
         self.dgamma, self.dbeta, self.dw1, self.dw2 = new(dim), new(dim), new(hidden, dim, dtype=dtype), new(dim, hidden, dtype=dtype)
         self.db1, self.db2 = new(hidden), new(dim)
         # between the passes
-        self._rstd, self._x, self._ready = new(rows), None, False
-        self._mean = None if keep8 else new(rows)
-        self._n8 = Packed.empty(rows, dim, device) if keep8 else None
-        self._z = Packed.empty(rows, hidden, device) if keep8 else new(rows, hidden, dtype=dtype)
+        self._x, self._now = None, None
+        mean, rstd = None if keep8 else new(rows), new(rows)
+        n8 = Packed.empty(rows, dim, device) if keep8 else None
+        z = Packed.empty(rows, hidden, device) if keep8 else new(rows, hidden, dtype=dtype)
         # within one
         scratch = scratch or BlockScratch(rows, dim, hidden, dtype, keep8, device)
         if (scratch.rows, scratch.dim, scratch.hidden, scratch.dtype) != (rows, dim, hidden, dtype) or scratch.keep8 < keep8:
             raise ValueError("the scratch is for blocks of other sizes or another type, or for ones that keep their activations whole")
-        self._dh, self._du, self._workspace = scratch.h, scratch.u, scratch.workspace
         # (the forward pass' h and u are free when it ends if they are kept in 8 bits)
-        self._h, self._u = (scratch.h, scratch.u) if keep8 else (new(rows, dim, dtype=dtype), new(rows, hidden, dtype=dtype))
+        h, u = (scratch.h, scratch.u) if keep8 else (new(rows, dim, dtype=dtype), new(rows, hidden, dtype=dtype))
+        self._all = (h, u, n8, z, mean, rstd, scratch.h, scratch.u, scratch.workspace)
+
+    def _of(self, rows):
+        """h, u, n8, z, mean, rstd, dh, du and the workspace of a pass of so many rows: the buffers' first ones.  (A call of fewer rows may split its sums into more
+        parts and so need more workspace; it takes its own.)"""
+        if rows == self.rows:
+            return self._all
+        if rows > self.rows:
+            raise ValueError(f"the block has room for {self.rows} rows")
+        return tuple(None if v is None else Packed(v.q[:rows], v.e[:rows], v.dim) if isinstance(v, Packed) else v[:rows] for v in self._all[:-1]) + (None,)
 
     def parameters(self):
         """[(parameter, gradient)]; the gradients are written by backward."""
         return [(self.gamma, self.dgamma), (self.beta, self.dbeta), (self.w1, self.dw1), (self.b1, self.db1), (self.w2, self.dw2), (self.b2, self.db2)]
 
     def forward(self, x, y):
-        """y of x, both float32 [rows, dim]; x has to stay until backward if activations are kept whole."""
-        self._ready = False                                # (a call that is refused half way leaves nothing for backward)
-        layer_norm(x, self.gamma, self.beta, self._h, self._mean, self._rstd, packed=self._n8, eps=self.eps)
-        linear(self._h, self.w1, self.b1, self._u, self.act, z=self._z, workspace=self._workspace)
-        linear(self._u, self.w2, self.b2, y, residual=x, workspace=self._workspace)
-        self._x, self._ready = None if self.keep8 else x, True
+        """y of x, both float32 [rows, dim] with as many rows as the block has or fewer; x has to stay until backward if activations are kept whole."""
+        self._now = None                                   # (a call that is refused half way leaves nothing for backward)
+        h, u, n8, z, mean, rstd, _, _, ws = now = self._of(len(x))
+        layer_norm(x, self.gamma, self.beta, h, mean, rstd, packed=n8, eps=self.eps)
+        linear(h, self.w1, self.b1, u, self.act, z=z, workspace=ws)
+        linear(u, self.w2, self.b2, y, residual=x, workspace=ws)
+        self._x, self._now = None if self.keep8 else x, now
 
     def backward(self, dy, dx):
-        """dx and the parameters' gradients from dy (float32 [rows, dim]), once for a forward pass.  dx may be dy itself."""
+        """dx and the parameters' gradients from dy (float32, as many rows as the forward pass had), once for a forward pass.  dx may be dy itself."""
         keep8 = self.keep8
-        if not self._ready:
+        if self._now is None:
             raise RuntimeError("backward follows a forward pass")
-        self._ready = False
+        (h, u, n8, z, mean, rstd, dh, du, ws), self._now = self._now, None
         # dz2 lies where dh will
-        linear_backward(dy, self._z if keep8 else self._u, self.w2, None, ACT_NONE, self._dh, self._du, self.dw2, self.db2,
-                        x_act=self.act if keep8 else ACT_NONE, workspace=self._workspace)
+        linear_backward(dy, z if keep8 else u, self.w2, None, ACT_NONE, dh, du, self.dw2, self.db2, x_act=self.act if keep8 else ACT_NONE, workspace=ws)
         # dz1 takes du's place: slope and product follow each other
-        linear_backward(self._du, self._n8 if keep8 else self._h, self.w1, self._z, self.act, self._du, self._dh, self.dw1, self.db1,
-                        x_gamma=self.gamma if keep8 else None, x_beta=self.beta if keep8 else None, workspace=self._workspace)
-        layer_norm_backward(self._dh, self._n8 if keep8 else self._x, self.gamma, self._mean, self._rstd, dx, self.dgamma, self.dbeta, residual=dy,
-                            workspace=self._workspace)
+        linear_backward(du, n8 if keep8 else h, self.w1, z, self.act, du, dh, self.dw1, self.db1, x_gamma=self.gamma if keep8 else None,
+                        x_beta=self.beta if keep8 else None, workspace=ws)
+        layer_norm_backward(dh, n8 if keep8 else self._x, self.gamma, mean, rstd, dx, self.dgamma, self.dbeta, residual=dy, workspace=ws)
         self._x = None

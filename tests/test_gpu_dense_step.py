@@ -195,3 +195,36 @@ def test_stacked_blocks_share_what_a_pass_alone_needs(keep8):
         with pytest.raises(ValueError):
             dense.ResidualBlock(rows, dim, hidden, t, keep8=True, scratch=scratch)
         dense.ResidualBlock(rows, dim, hidden, t, keep8=False, scratch=dense.BlockScratch(rows, dim, hidden, t))
+
+
+@pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("keep8", [False, True])
+def test_a_batch_of_fewer_rows(keep8, t):
+    """The last batch of an epoch through the same block: the bits of a block made for so many rows (with the same weights), and whole batches before and after it."""
+    rows, dim, hidden = 700, 96, 160
+    dev = torch.device("cuda:0")
+
+    def block(rows):
+        g = torch.Generator(device=dev)
+        g.manual_seed(6)
+        return dense.ResidualBlock(rows, dim, hidden, t, keep8=keep8, generator=g)
+
+    def run(b, rows):
+        g = torch.Generator(device=dev)
+        g.manual_seed(rows + 1)
+        x, dy = [torch.randn(rows, dim, generator=g, device=dev) for _ in range(2)]
+        y, dx = torch.empty_like(x), torch.empty_like(x)
+        b.forward(x, y)
+        b.backward(dy, dx)
+        return [y, dx] + [d.clone() for _, d in b.parameters()]
+
+    b = block(rows)
+    for some in (rows, 1, 333, 257, 0, rows - 1, 16, rows):
+        for got, want in zip(run(b, some), run(block(some), some)):
+            assert torch.equal(got, want)
+    x = torch.zeros(rows + 1, dim, device=dev)
+    with pytest.raises(ValueError):
+        b.forward(x, torch.empty_like(x))
+    b.forward(x[:9], torch.empty(9, dim, device=dev))
+    with pytest.raises(ValueError):                       # as many as the forward pass had
+        b.backward(x[:8], torch.empty(8, dim, device=dev))
