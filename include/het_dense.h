@@ -22,7 +22,8 @@
  *   q  int8[rows][pitch]        whole steps, in [-127, 127]; zero behind the row's end
  *   e  uint8[rows][pitch / 32]  a block of 32 values of a row shares the step 2^(e - 127)
  * e is the smallest for which the block's largest magnitude rounds to at most 127 steps (ties to even; 1 <= e <= 249), so a value is off
- * by at most half a step, 1/127 of that magnitude.  A block that holds an infinity or a NaN has e = 255 and stands for NaN
+ * by at most half a step, 1/127 of that magnitude.  (With e = 249, of magnitudes from 63.75 2^122 on, q is at most 63, since 64 steps would be
+ * beyond fp32: a value there is off by less than a step.)  A block that holds an infinity or a NaN has e = 255 and stands for NaN
  * everywhere.  What is kept takes 8.25 bits a value, and is exactly representable in bf16.  q must be aligned to 16 bytes.
  */
 #ifndef HET_DENSE_H
@@ -130,7 +131,8 @@ int het_linear(const het_linear_t *l, void *hip_stream);
  * workspace as het_expand does.  relu's slope at 0 is 0; an infinite z (a sum
  * beyond fp16's range kept in fp16) has its slope's limit, 1 or 0.  dz may be NULL if it would be dy itself (no activation, y_type == type), and
  * may be dy itself if the types are the same.  With rows == 0, dw and dbias are zero.
- * workspace: het_linear_workspace(l, 1) bytes, aligned to 16.  HET_EINVAL as above.
+ * workspace: het_linear_workspace(l, 1) bytes, aligned to 16.  HET_EINVAL as above, and: a dw of too many values for one launch
+ * (2^38 and more may be; 2^40 are).
  */
 int het_linear_backward(const het_linear_t *l, void *hip_stream);
 

@@ -135,3 +135,13 @@ def test_layer_norm_backward_of_no_rows_kept_in_8_bits():
     lib = dense.load()
     assert back(lib, rows=0, dy=None, x=None, ldx=0, dx=None, mean=None, rstd=None, dgamma=None, dbeta=None) == HET_OK
     assert back(lib, rows=1, ldx=0) == HET_EINVAL
+
+
+def test_a_gradient_of_too_many_values_for_a_launch_is_refused():
+    """dw of 2^40 values, with all of the workspace that is named for it."""
+    lib = dense.load()
+    n = 1 << 20
+    big = dict(rows=8, inp=n, out=n, ldx=n, ldw=n, lddx=n, lddw=n, lddy=n, lddz=n, act=0, zq=None, ze=None)
+    need = lib.het_linear_workspace(linear_args(**big), 1)
+    assert need >= 0
+    assert lib.het_linear_backward(linear_args(**big, workspace_bytes=need), None) == HET_EINVAL
