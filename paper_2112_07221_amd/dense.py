@@ -164,7 +164,11 @@ def _packed(p, what, rows, dim, dev):
 
 
 def _stream(stream, dev):
-    return _raw_stream(dev) if stream is None else stream.cuda_stream
+    if stream is None:
+        return _raw_stream(dev)
+    if stream.device_index != dev:
+        raise ValueError("stream is on another device than the current one")
+    return stream.cuda_stream
 
 
 def _scratch(need, workspace, stream, dev):

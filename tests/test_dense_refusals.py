@@ -145,3 +145,12 @@ def test_a_gradient_of_too_many_values_for_a_launch_is_refused():
     need = lib.het_linear_workspace(linear_args(**big), 1)
     assert need >= 0
     assert lib.het_linear_backward(linear_args(**big, workspace_bytes=need), None) == HET_EINVAL
+
+
+def test_a_stream_of_another_device_is_refused():
+    class Stream:
+        cuda_stream, device_index = 40, 1
+
+    assert dense._stream(Stream, 1) == 40
+    with pytest.raises(ValueError):
+        dense._stream(Stream, 0)
