@@ -126,7 +126,9 @@ __global__ __launch_bounds__(MOST) void norm_kernel(NormArgs a)
         const f32x8 b = a.beta ? load_row<WHOLE>(a.beta, c, dim) : f32x8{};
 #pragma unroll
         for (int j = 0; j < 8; ++j) h[j] = h[j] * g[j] + b[j];
-        store_row<WHOLE, true>(y, c, dim, h);         // (past the L2: 106496 x 64 to bf16 and 8 bits, expanded, 17.0 -> 16.3 us)
+        // Past the L2: 106496 x 64 to bf16 alone 6.3 us (through it 7.8), 4096 x 1664 8.2 (9.4).  With the product that reads them: 2048 x 1664 -> 4096 37.2 (39.1),
+        // 4096 x 1664 -> 4096 61.4 (60.9), 16384 x 896 -> 4096 141.3 (138.9), 106496 x 64 -> 64 25.6 (22.7); below 1024 x 1664 values no difference.
+        store_row<WHOLE, true>(y, c, dim, h);
     }
 }
 
